@@ -94,6 +94,9 @@ extern "C" {
 #define QKV_STATUS_BAD_COUNTS   0x2u  /* counts[] passed by the host differ from the histogram */
 #define QKV_STATUS_BAD_HEADER   0x4u  /* unpack: magic / version / shape / sizes do not match  */
 #define QKV_STATUS_BAD_ORDER    0x8u  /* an order[] entry was >= tokens (row skipped / zeros)  */
+#define QKV_STATUS_BAD_PAGE     0x10u /* a table entry that was needed names no page (its tokens are not seen / written) */
+#define QKV_STATUS_BAD_ROW      0x20u /* a row number, a length or a row's place in a batch is not what it may be        */
+#define QKV_STATUS_NO_PAGES     0x40u /* fewer free pages than the call needs (nothing was changed)                      */
 
 /* Problem description, host memory, caller-owned (paper Sec. 3.1 shape, Sec. 4.2.1 metadata). */
 typedef struct qkv_desc {
@@ -486,6 +489,148 @@ int qkv_card_attend_kc(const void* card_dev, uint64_t card_bytes, const qkv_desc
 int qkv_card_attend_static(const void* card_dev, uint64_t card_bytes, const qkv_desc_t* expect,
                            const void* q_dev, int32_t q_heads, float softmax_scale,
                            float* out_dev, float* lse_dev, uint32_t* status_dev, void* stream);
+
+/*
+ * A receiver's own cache, in pages, and the attention that reads it (paper Sec. 4.2.2: the receiver goes on from the injected cache
+ * with tokens of its own; Sec. 4.3: attention over a card gives (out, lse), to be joined with attention over those tokens).
+ * Several agents can go on from one injected context: their rows share its pages.
+ *
+ * The pool: per layer one tensor of keys and one of values, `pages` pages of page_tokens tokens.  Token i of page p, kv head h, starts
+ * p * page_stride + h * head_stride + i * token_stride elements behind the layer's pointer and is one contiguous row of head_dim
+ * 16-bit values.  Which sequence holds what is device memory of the caller's:
+ *   lens_dev   [rows]              tokens of each sequence; 0 for a place that is not in use
+ *   table_dev  [rows][row_pages]   entry j of a row: the page of tokens j * page_tokens and on.  Entries behind the last page a
+ *                                  length needs mean nothing and are never looked at.
+ *   refs_dev   [pages]             how many entries name the page; 0 is free.  Only qkv_pages_reserve / _fork / _free / _compact need it.
+ * A page whose last tokens are not written yet belongs to one row only; the calls below keep it so.
+ * The pointer arrays are host memory, read before a call returns.
+ *
+ * Shapes: layers 1 .. 64; head_dim 64, 128, 256; page_tokens a power of two up to 2^20; pages < 2^31; rows <= 65536; row_pages * page_tokens
+ * (room for one sequence) and rows * row_pages < 2^31; strides multiples of 8 elements below 2^31, token_stride >= head_dim; layer
+ * pointers 16-byte aligned, others 4 (QKV_ERR_SHAPE, QKV_ERR_ALIGN).  The library cannot see the tensors' extents.
+ *
+ * What only the device sees never makes a call leave these tensors: lengths count as 0 .. row_pages * page_tokens, an entry that names no
+ * page is QKV_STATUS_BAD_PAGE.  Status words: qkv_pages_reserve, _fork and _compact need one and set it (0 when all is well); the
+ * other calls or their bits into it, where one is given, and clear nothing.
+ * All calls are asynchronous on `stream` and allocate nothing.  Calls that share a pool belong on one stream, or are ordered by the caller.
+ */
+#define QKV_VALUE_FP16 0
+#define QKV_VALUE_BF16 1
+
+typedef struct qkv_pages {
+  int32_t layers, kv_heads, head_dim, page_tokens;
+  int32_t value_type;                 /* QKV_VALUE_* of keys, values and queries */
+  int32_t pages, rows, row_pages;
+  void* const* k_layers;              /* host array [layers] of device pointers */
+  void* const* v_layers;
+  int64_t page_stride, head_stride, token_stride;   /* in elements */
+  int32_t* table_dev;
+  int32_t* lens_dev;
+  int32_t* refs_dev;                  /* NULL where it is not needed */
+} qkv_pages_t;
+
+/*
+ * Makes room for new tokens: row i grows by more_dev[i] (device, int32_t[rows]; NULL: every row by 1).  Rows take new pages in their
+ * order, the lowest free page first, and lens_dev holds the new lengths afterwards; qkv_pages_append then writes the tokens.
+ * All or nothing: with a negative number, a length that the row has no entries for (QKV_STATUS_BAD_ROW) or too few free pages
+ * (QKV_STATUS_NO_PAGES) nothing changes.
+ */
+int qkv_pages_reserve(const qkv_pages_t* pages, const int32_t* more_dev, uint32_t* status_dev, void* stream);
+
+/*
+ * Rows of new tokens into the pages of the sequences' last places.  Token i of row b, i = starts_dev[b] .. starts_dev[b + 1] - 1 of the
+ * batch, goes to place lens_dev[b] - (starts_dev[b + 1] - starts_dev[b]) + (i - starts_dev[b]): lengths count the new tokens already.
+ *   starts_dev: device, int32_t[rows + 1], rising; NULL: one token for every row (tokens == rows), which a row of length 0 leaves out.
+ *   k_dev, v_dev: device, the new rows: layer l (counted from layer_begin), token i, head h start l * layer_stride + i * token_stride +
+ *             h * head_stride elements behind it; strides multiples of 8, below 2^40, pointers 16-byte aligned.  A dense cache of
+ *             qkv_unpack_dequant goes in with layer_stride = H*T*D, head_stride = T*D, token_stride = D.
+ * Tokens behind the last row's are left out.  A place in front of the sequence or behind its entries is QKV_STATUS_BAD_ROW, and nothing is written.
+ */
+typedef struct qkv_rows {
+  const void* k_dev;
+  const void* v_dev;
+  int64_t tokens;
+  int64_t layer_stride, head_stride, token_stride;
+  const int32_t* starts_dev;
+  int32_t layer_begin, layer_count;
+} qkv_rows_t;
+
+int qkv_pages_append(const qkv_pages_t* pages, const qkv_rows_t* rows, uint32_t* status_dev, void* stream);
+
+/*
+ * Sequences that go on from another one: row target_dev[i] becomes what row source_dev[i] is (device, int32_t[count], 1 <= count <= rows).
+ * What the targets held is given back first.  Full pages are shared; a last page that is not full is copied (its tokens, in all layers) to a
+ * new page, the lowest free one, in the order of the pairs.  Targets are all different and none is a source, else
+ * QKV_STATUS_BAD_ROW; with too few free pages QKV_STATUS_NO_PAGES; in both cases nothing has changed when the call's work is done.
+ */
+int qkv_pages_fork(const qkv_pages_t* pages, const int32_t* source_dev, const int32_t* target_dev, int32_t count, uint32_t* status_dev,
+                   void* stream);
+
+/*
+ * Pages given back by rows rows_dev[0 .. count) (NULL: all rows, count == rows).  window == 0: the rows hold nothing afterwards, lengths
+ * are 0.  window > 0: only pages none of whose tokens a query at the row's last place or later sees (see qkv_paged_attend); their
+ * entries become -1, lengths stay.  A row that is listed twice counts once; one that is none is QKV_STATUS_BAD_ROW.
+ */
+int qkv_pages_free(const qkv_pages_t* pages, const int32_t* rows_dev, int32_t count, int32_t window, int32_t sinks, uint32_t* status_dev,
+                   void* stream);
+
+/*
+ * Moves the pages in use (refs > 0) to the pages 0 .. n - 1: the k-th page in use from n on goes to the k-th free page below n, in all layers;
+ * entries and refs follow, live_dev (device, may be NULL) gets n.  Pages moved from keep their contents.
+ * workspace_dev: device scratch of qkv_pages_compact_workspace() bytes, 16-byte aligned, contents unspecified (QKV_ERR_CAPACITY if smaller).
+ */
+int qkv_pages_compact_workspace(const qkv_pages_t* pages, uint64_t* bytes_out);
+int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,
+                      void* stream);
+
+/*
+ * Attention over the pages of one layer.  With R = q_heads / kv_heads (at most QKV_PAGED_MAX_REP) query head hq reads kv head hq / R; a query
+ * at place p of its sequence sees the tokens t <= p and, with window > 0, of those only t > p - window and t < sinks:
+ *     s_t = softmax_scale * <q, K_t>,   out = sum_t softmax(s)_t * V_t,   lse = log sum_t exp(s_t)
+ * A query that sees nothing has out = 0, lse = -inf.  Tokens that are not seen count for nothing, whatever their rows hold.
+ *   q_dev:    device, values of the pages' type: query i, head hq start i * q_token_stride + hq * q_head_stride elements behind it; strides
+ *             multiples of 8, 16-byte aligned, so a part of a fused projection's result will do.
+ *   lse_dev:  device, float [tokens][q_heads], may be NULL.
+ *   workspace_dev: device scratch, 16-byte aligned, contents unspecified, of the bytes the call's _workspace function names; NULL where
+ *             that is 0.  Two calls that may run at once, graphs among them, need one each.
+ *
+ * qkv_paged_attend: one new token of every sequence, p = lens_dev[i] - 1; tokens == rows, starts_dev NULL.  out is float
+ * [rows][q_heads][head_dim], 16-byte aligned.  prior_out / prior_lse (float, shapes of out / lse, both or neither): the result of
+ * attention over tokens that are somewhere else, qkv_card_attend's over a card above all; out and lse are then those of both together.
+ * (prior_out may be out itself, and prior_lse lse.)  All sums in fp32, weights held to 22 bits or more.
+ *
+ * qkv_paged_prompt: many new tokens, whose keys and values are in the pages already: token i of row b (starts_dev as for qkv_pages_append,
+ * here required, tokens >= 1) stands at place lens_dev[b] - n_b + (i - starts_dev[b]).  out is of the pages' type,
+ * [tokens][q_heads][head_dim]; weights are rounded to that type for the product with the values, sums and lse are fp32.  out and lse of tokens
+ * behind the last row's are left as they were; a row with more new tokens than length is QKV_STATUS_BAD_ROW (those in front see nothing).
+ *
+ * Errors: QKV_ERR_NULL, QKV_ERR_SHAPE (also: window < 0, sinks without a window, a scale that is not finite), QKV_ERR_ALIGN,
+ * QKV_ERR_CAPACITY, QKV_ERR_HIP.
+ */
+#define QKV_PAGED_MAX_REP 128
+
+typedef struct qkv_paged_query {
+  const void* q_dev;
+  int64_t q_token_stride, q_head_stride;   /* in elements */
+  int64_t tokens;
+  const int32_t* starts_dev;
+  void* out_dev;
+  float* lse_dev;
+  const float* prior_out_dev;
+  const float* prior_lse_dev;
+  void* workspace_dev;
+  uint64_t workspace_bytes;
+  uint32_t* status_dev;
+  int32_t layer, q_heads;
+  int32_t window, sinks;
+  float softmax_scale;
+  int32_t reserved;                        /* 0 */
+} qkv_paged_query_t;
+
+int qkv_paged_attend_workspace(const qkv_pages_t* pages, int32_t q_heads, uint64_t* bytes_out);
+int qkv_paged_attend(const qkv_pages_t* pages, const qkv_paged_query_t* query, void* stream);
+int qkv_paged_prompt_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_t tokens, uint64_t* bytes_out);
+int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, void* stream);
 
 /*
  * Read a card's header back to the host (paper Sec. 4.2.1: the card is self-describing - sequence length, identifiers,

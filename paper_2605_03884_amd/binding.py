@@ -11,6 +11,9 @@ STATUS_BAD_BITS = 0x1
 STATUS_BAD_COUNTS = 0x2
 STATUS_BAD_HEADER = 0x4
 STATUS_BAD_ORDER = 0x8
+STATUS_BAD_PAGE = 0x10
+STATUS_BAD_ROW = 0x20
+STATUS_NO_PAGES = 0x40
 FLAG_KEYS_PER_CHANNEL = 0x1
 
 
@@ -75,6 +78,72 @@ class _InjectByAddress(ctypes.Structure):
     """qkv_inject_t with the tables' addresses as numbers."""
     _fields_ = [(name, ctypes.c_size_t if name in ("k_layers", "v_layers") else kind) for name, kind in Inject._fields_]
 
+
+class Pages(ctypes.Structure):
+    """qkv_pages_t, and the tensors it points to, which it keeps alive."""
+    _fields_ = [
+        ("layers", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+        ("value_type", ctypes.c_int32), ("pages", ctypes.c_int32), ("rows", ctypes.c_int32), ("row_pages", ctypes.c_int32),
+        ("k_layers", ctypes.POINTER(ctypes.c_void_p)), ("v_layers", ctypes.POINTER(ctypes.c_void_p)),
+        ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+        ("table_dev", ctypes.c_void_p), ("lens_dev", ctypes.c_void_p), ("refs_dev", ctypes.c_void_p),
+    ]
+
+    @classmethod
+    def make(cls, k_layers, v_layers, table, lens, refs=None):
+        """k_layers, v_layers: lists of device float16 or bfloat16 tensors (views are fine) [pages, kv_heads, page_tokens, head_dim], rows
+        contiguous, all with the same strides; table: device int32 [rows, row_pages]; lens: device int32 [rows]; refs: device int32 [pages]
+        (needed by pages_reserve, pages_fork, pages_free and pages_compact)."""
+        count = len(k_layers)
+        if count < 1 or count != len(v_layers):
+            raise ValueError("k_layers and v_layers must be lists of the same, non-zero length")
+        first = k_layers[0]
+        if first.dtype not in _VALUE_TYPES:
+            raise ValueError("pages must be float16 or bfloat16")
+        for t in (*k_layers, *v_layers):
+            if t.dim() != 4 or t.dtype != first.dtype or t.shape != first.shape or t.device != first.device or not t.is_cuda:
+                raise ValueError("layer tensors must be device tensors [pages, kv_heads, page_tokens, head_dim] of one type, shape and device")
+            if t.stride() != first.stride() or t.stride(3) != 1:
+                raise ValueError("layer tensors must share their strides and have contiguous rows")
+        for t, shape, name in ((table, None, "table"), (lens, (table.shape[0],), "lens"), (refs, (first.shape[0],), "refs")):
+            if t is None and name == "refs":
+                continue
+            _dev_ptr(t, torch.int32, name)
+            if t.device != first.device:
+                raise ValueError("%s must live on the pages' device" % name)
+            if t.dim() != 2 if shape is None else tuple(t.shape) != shape:
+                raise ValueError("%s has the wrong shape" % name)
+        pointers = (ctypes.c_void_p * (2 * count))(*[t.data_ptr() for t in (*k_layers, *v_layers)])
+        values = ctypes.cast(ctypes.addressof(pointers) + 8 * count, ctypes.POINTER(ctypes.c_void_p))
+        p = cls(count, first.shape[1], first.shape[3], first.shape[2], _VALUE_TYPES[first.dtype], first.shape[0], table.shape[0], table.shape[1],
+                ctypes.cast(pointers, ctypes.POINTER(ctypes.c_void_p)), values, first.stride(0), first.stride(1), first.stride(2),
+                table.data_ptr(), lens.data_ptr(), None if refs is None else refs.data_ptr())
+        p.tensors = (list(k_layers), list(v_layers), table, lens, refs, pointers)
+        p.dtype, p.device = first.dtype, first.device
+        return p
+
+
+class Rows(ctypes.Structure):
+    """qkv_rows_t."""
+    _fields_ = [
+        ("k_dev", ctypes.c_size_t), ("v_dev", ctypes.c_size_t), ("tokens", ctypes.c_int64),
+        ("layer_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("token_stride", ctypes.c_int64),
+        ("starts_dev", ctypes.c_size_t), ("layer_begin", ctypes.c_int32), ("layer_count", ctypes.c_int32),
+    ]
+
+
+class PagedQuery(ctypes.Structure):
+    """qkv_paged_query_t."""
+    _fields_ = [
+        ("q_dev", ctypes.c_size_t), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("tokens", ctypes.c_int64),
+        ("starts_dev", ctypes.c_size_t), ("out_dev", ctypes.c_size_t), ("lse_dev", ctypes.c_size_t), ("prior_out_dev", ctypes.c_size_t),
+        ("prior_lse_dev", ctypes.c_size_t), ("workspace_dev", ctypes.c_size_t), ("workspace_bytes", ctypes.c_uint64),
+        ("status_dev", ctypes.c_size_t), ("layer", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("window", ctypes.c_int32),
+        ("sinks", ctypes.c_int32), ("softmax_scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+_VALUE_TYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 _pointer_tables = [ctypes.c_void_p * (2 * count) for count in range(5)]
 
@@ -148,6 +217,19 @@ def lib():
     L.qkv_card_attend_static.restype = ctypes.c_int
     L.qkv_card_attend_static.argtypes = [vp, ctypes.c_uint64, ctypes.POINTER(Desc), vp, ctypes.c_int32, ctypes.c_float, vp, vp,
                                          vp, vp]
+    pages, bytes_out = ctypes.POINTER(Pages), ctypes.POINTER(ctypes.c_uint64)
+    for name, args in (("pages_reserve", [pages, vp, vp, vp]),
+                       ("pages_append", [pages, ctypes.POINTER(Rows), vp, vp]),
+                       ("pages_fork", [pages, vp, vp, ctypes.c_int32, vp, vp]),
+                       ("pages_free", [pages, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]),
+                       ("pages_compact_workspace", [pages, bytes_out]),
+                       ("pages_compact", [pages, vp, vp, ctypes.c_uint64, vp, vp]),
+                       ("paged_attend_workspace", [pages, ctypes.c_int32, bytes_out]),
+                       ("paged_attend", [pages, ctypes.POINTER(PagedQuery), vp]),
+                       ("paged_prompt_workspace", [pages, ctypes.c_int32, ctypes.c_int64, bytes_out]),
+                       ("paged_prompt", [pages, ctypes.POINTER(PagedQuery), vp])):
+        entry = getattr(L, "qkv_" + name)
+        entry.restype, entry.argtypes = ctypes.c_int, args
     L.qkv_card_peek.restype = ctypes.c_int
     L.qkv_card_peek.argtypes = [vp, ctypes.c_uint64, ctypes.POINTER(Desc), i64p, ctypes.POINTER(ctypes.c_float),
                                 ctypes.POINTER(ctypes.c_uint32), vp]
@@ -456,3 +538,131 @@ def card_peek(card, card_nbytes=None, stream=None):
     _check(lib().qkv_card_peek(_dev_ptr(card, torch.uint8, "card"), n, ctypes.byref(d), counts, ctypes.byref(avg),
                                ctypes.byref(st), _stream(stream)), "qkv_card_peek")
     return d, list(counts), avg.value, st.value
+
+
+def _here(pages, stream):
+    """The stream's handle; the current stream of the pages' device without one.  Calls go to the current device: it has to be the pages'."""
+    if pages.device.index != _current_device():
+        raise ValueError("the pages live on %s: make it the current device" % pages.device)
+    return _stream(stream)
+
+
+def _of_pages(t, pages, dtype, shape, name):
+    """The address of a contiguous tensor on the pages' device."""
+    if t.device != pages.device or t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor %s on %s" % (name, dtype, list(shape), pages.device))
+    return t.data_ptr()
+
+
+def _status_of_pages(status, pages):
+    if status is None:
+        return 0
+    if status.device != pages.device or status.numel() < 1 or status.dtype.itemsize != 4:
+        raise ValueError("status must be one 32-bit word on %s" % pages.device)
+    return status.data_ptr()
+
+
+def pages_reserve(pages, more, status, stream=None):
+    """Room for more[i] (device int32 [rows]; None: 1 each) new tokens in every row; lens are the new lengths afterwards."""
+    at = None if more is None else _of_pages(more, pages, torch.int32, (pages.rows,), "more")
+    _check(lib().qkv_pages_reserve(pages, at, _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_reserve")
+
+
+def pages_append(pages, k, v, layer=0, starts=None, status=None, stream=None):
+    """k, v: device tensors of the pages' type [layers, tokens, kv_heads, head_dim] or, of one layer, [tokens, kv_heads, head_dim] (views with
+    contiguous rows are fine, both with the same strides) into the pages of layer `layer` and on; starts: device int32 [rows + 1], or None for
+    one token a row.  A dense cache [layers, kv_heads, tokens, head_dim] is passed as .transpose(1, 2)."""
+    if k.dim() == 3:
+        k, v = k.unsqueeze(0), v.unsqueeze(0)
+    shape, strides = k.shape, k.stride()
+    if len(shape) != 4 or v.shape != shape or v.stride() != strides or strides[3] != 1 or shape[2] != pages.kv_heads or shape[3] != pages.head_dim:
+        raise ValueError("k and v must be [layers, tokens, kv_heads, head_dim] with the same strides and contiguous rows")
+    if k.dtype is not pages.dtype or v.dtype is not pages.dtype or k.device != pages.device or v.device != pages.device:
+        raise ValueError("k and v must have the pages' type and device")
+    if shape[1] == 0:
+        return
+    at = 0 if starts is None else _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
+    rows = Rows(k.data_ptr(), v.data_ptr(), shape[1], strides[0], strides[2], strides[1], at, layer, shape[0])
+    _check(lib().qkv_pages_append(pages, rows, _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_append")
+
+
+def pages_fork(pages, source, target, status, stream=None):
+    """Rows target[i] go on from rows source[i] (device int32 [n])."""
+    n = source.numel()
+    _check(lib().qkv_pages_fork(pages, _of_pages(source, pages, torch.int32, (n,), "source"), _of_pages(target, pages, torch.int32, (n,), "target"), n,
+                                _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_fork")
+
+
+def pages_free(pages, rows=None, window=0, sinks=0, status=None, stream=None):
+    """Gives back the pages of the rows (device int32 [n]; None: all), with a window only those that are out of sight for good."""
+    n = pages.rows if rows is None else rows.numel()
+    at = None if rows is None else _of_pages(rows, pages, torch.int32, (n,), "rows")
+    _check(lib().qkv_pages_free(pages, at, n, int(window), int(sinks), _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_free")
+
+
+def pages_compact_workspace(pages):
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_pages_compact_workspace(pages, ctypes.byref(out)), "qkv_pages_compact_workspace")
+    return out.value
+
+
+def pages_compact(pages, status, live=None, workspace=None, stream=None):
+    """Moves the pages in use to the front of the pool; live: device int32 [1] for their number, or None."""
+    if workspace is None:
+        workspace = torch.empty(pages_compact_workspace(pages), dtype=torch.uint8, device=pages.device)
+    lp = None if live is None else _of_pages(live, pages, torch.int32, (1,), "live")
+    _check(lib().qkv_pages_compact(pages, lp, _of_pages(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel(),
+                                   _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_compact")
+
+
+def _paged_query(pages, q, softmax_scale, out, out_type, lse, layer, window, sinks, workspace, status):
+    shape, strides = q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != pages.head_dim or strides[2] != 1 or q.dtype is not pages.dtype or q.device != pages.device:
+        raise ValueError("q must be [tokens, q_heads, head_dim] of the pages' type and device, rows contiguous")
+    x = PagedQuery(q.data_ptr(), strides[0], strides[1], shape[0])
+    x.out_dev = _of_pages(out, pages, out_type, shape, "out")
+    if lse is not None:
+        x.lse_dev = _of_pages(lse, pages, torch.float32, shape[:2], "lse")
+    if workspace is not None:
+        x.workspace_dev, x.workspace_bytes = _of_pages(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel()
+    if status is not None:
+        x.status_dev = _status_of_pages(status, pages)
+    x.layer, x.q_heads, x.window, x.sinks, x.softmax_scale = layer, shape[1], window, sinks, softmax_scale
+    return x
+
+
+def paged_attend_workspace(pages, q_heads):
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_paged_attend_workspace(pages, int(q_heads), ctypes.byref(out)), "qkv_paged_attend_workspace")
+    return out.value
+
+
+def paged_attend(pages, q, softmax_scale, out, lse=None, layer=0, window=0, sinks=0, prior=None, workspace=None, status=None, stream=None):
+    """Attention of one new token of every row over its pages.  q: device [rows, q_heads, head_dim] of the pages' type (a view with contiguous
+    rows is fine); out: device float32 of the same shape; lse: float32 [rows, q_heads]; prior: (out, lse) of attention over other tokens
+    (card_attend's), which the result then covers too."""
+    if workspace is None:
+        workspace = torch.empty(paged_attend_workspace(pages, q.shape[1]), dtype=torch.uint8, device=pages.device)
+    x = _paged_query(pages, q, softmax_scale, out, torch.float32, lse, layer, window, sinks, workspace, status)
+    if prior is not None:
+        x.prior_out_dev = _of_pages(prior[0], pages, torch.float32, q.shape, "prior[0]")
+        x.prior_lse_dev = _of_pages(prior[1], pages, torch.float32, q.shape[:2], "prior[1]")
+    _check(lib().qkv_paged_attend(pages, x, _here(pages, stream)), "qkv_paged_attend")
+    return out, lse
+
+
+def paged_prompt_workspace(pages, q_heads, tokens):
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_paged_prompt_workspace(pages, int(q_heads), int(tokens), ctypes.byref(out)), "qkv_paged_prompt_workspace")
+    return out.value
+
+
+def paged_prompt(pages, q, starts, softmax_scale, out, lse=None, layer=0, window=0, sinks=0, workspace=None, status=None, stream=None):
+    """Attention of the rows' last tokens, those of row i at q[starts[i]:starts[i + 1]], each over what stands up to its own place.
+    q: device [tokens, q_heads, head_dim] of the pages' type; starts: device int32 [rows + 1]; out: of the pages' type; lse: float32 [tokens, q_heads]."""
+    if workspace is None:
+        workspace = torch.empty(paged_prompt_workspace(pages, q.shape[1], q.shape[0]), dtype=torch.uint8, device=pages.device)
+    x = _paged_query(pages, q, softmax_scale, out, pages.dtype, lse, layer, window, sinks, workspace, status)
+    x.starts_dev = _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
+    _check(lib().qkv_paged_prompt(pages, x, _here(pages, stream)), "qkv_paged_prompt")
+    return out, lse

@@ -1,0 +1,320 @@
+// paged_api.hip — the C ABI of the cache in pages: argument checks and launch planning.
+#include <cmath>
+
+#include "paged.h"
+
+using namespace qkv;
+
+namespace {
+
+constexpr uint32_t kAttendShares = 4096;      // shares of the decode kernel's work at most: waves that fit the chip at four a SIMD
+constexpr uint32_t kPromptRows = 128;         // (query token, query head) pairs of a prompt tile
+constexpr uint32_t kPromptTarget = 512;       // workgroups the prompt kernel's work is split into, where there are fewer query tiles
+
+bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
+
+int check_pages(const qkv_pages_t* p, bool counted) {
+  if (!p || !p->k_layers || !p->v_layers || !p->table_dev || !p->lens_dev || (counted && !p->refs_dev)) return QKV_ERR_NULL;
+  if (p->layers < 1 || p->layers > QKV_INJECT_MAX_LAYERS || p->kv_heads < 1 || p->kv_heads > (1 << 16)) return QKV_ERR_SHAPE;
+  if (p->head_dim != 64 && p->head_dim != 128 && p->head_dim != 256) return QKV_ERR_SHAPE;
+  if (p->page_tokens < 1 || p->page_tokens > (1 << 20) || (p->page_tokens & (p->page_tokens - 1)) != 0) return QKV_ERR_SHAPE;
+  if (p->value_type != QKV_VALUE_FP16 && p->value_type != QKV_VALUE_BF16) return QKV_ERR_SHAPE;
+  if (p->pages < 1 || p->rows < 1 || p->rows > (int32_t)kMaxRows || p->row_pages < 1) return QKV_ERR_SHAPE;
+  if ((int64_t)p->row_pages * p->page_tokens >= (1ll << 31) - p->page_tokens || (int64_t)p->rows * p->row_pages >= (1ll << 31)) return QKV_ERR_SHAPE;
+  const int64_t strides[3] = {p->page_stride, p->head_stride, p->token_stride};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 31)) return QKV_ERR_SHAPE;
+  if (p->token_stride < p->head_dim) return QKV_ERR_SHAPE;
+  if ((int64_t)p->page_tokens * p->kv_heads * p->head_dim >= (1ll << 31)) return QKV_ERR_SHAPE;     // a page's own size counts in 32 bits
+  if (misaligned(p->table_dev, 4) || misaligned(p->lens_dev, 4) || misaligned(p->refs_dev, 4)) return QKV_ERR_ALIGN;
+  for (int i = 0; i < p->layers; ++i) {
+    if (!p->k_layers[i] || !p->v_layers[i]) return QKV_ERR_NULL;
+    if (misaligned(p->k_layers[i], 16) || misaligned(p->v_layers[i], 16)) return QKV_ERR_ALIGN;
+  }
+  return QKV_OK;
+}
+
+uint32_t log2_of(int32_t power) { return (uint32_t)__builtin_ctz((unsigned)power); }
+
+PageCache cache_of(const qkv_pages_t* p) {
+  PageCache c = {};
+  for (int i = 0; i < p->layers; ++i) {
+    c.k[i] = static_cast<uint8_t*>(p->k_layers[i]);
+    c.v[i] = static_cast<uint8_t*>(p->v_layers[i]);
+  }
+  c.page_stride = (uint64_t)p->page_stride * 2u;
+  c.head_stride = (uint64_t)p->head_stride * 2u;
+  c.token_stride = (uint64_t)p->token_stride * 2u;
+  c.table = p->table_dev;
+  c.lens = p->lens_dev;
+  c.refs = p->refs_dev;
+  c.layers = (uint32_t)p->layers;
+  c.kv_heads = (uint32_t)p->kv_heads;
+  c.head_dim = (uint32_t)p->head_dim;
+  c.page_shift = log2_of(p->page_tokens);
+  c.pages = (uint32_t)p->pages;
+  c.rows = (uint32_t)p->rows;
+  c.row_pages = (uint32_t)p->row_pages;
+  return c;
+}
+
+PageLayer layer_of(const qkv_pages_t* p, int32_t layer) {
+  PageLayer l;
+  l.k = static_cast<const uint8_t*>(p->k_layers[layer]);
+  l.v = static_cast<const uint8_t*>(p->v_layers[layer]);
+  l.page_stride = (uint64_t)p->page_stride * 2u;
+  l.head_stride = (uint64_t)p->head_stride * 2u;
+  l.token_stride = (uint64_t)p->token_stride * 2u;
+  l.table = p->table_dev;
+  l.lens = p->lens_dev;
+  l.rows = (uint32_t)p->rows;
+  l.row_pages = (uint32_t)p->row_pages;
+  l.pages = (uint32_t)p->pages;
+  l.page_shift = log2_of(p->page_tokens);
+  l.kv_heads = (uint32_t)p->kv_heads;
+  return l;
+}
+
+int check_heads(const qkv_pages_t* p, int32_t q_heads) {
+  if (q_heads < p->kv_heads || q_heads % p->kv_heads != 0 || q_heads / p->kv_heads > QKV_PAGED_MAX_REP) return QKV_ERR_SHAPE;
+  return QKV_OK;
+}
+
+int check_where(const qkv_pages_t* p, const qkv_paged_query_t* a) {
+  if (!a->q_dev || !a->out_dev) return QKV_ERR_NULL;
+  if (a->layer < 0 || a->layer >= p->layers) return QKV_ERR_SHAPE;
+  const int rc = check_heads(p, a->q_heads);
+  if (rc) return rc;
+  if (a->q_token_stride < 0 || a->q_token_stride % 8 != 0 || a->q_token_stride >= (1ll << 40) || a->q_head_stride < 0 || a->q_head_stride % 8 != 0 ||
+      a->q_head_stride >= (1ll << 31))
+    return QKV_ERR_SHAPE;
+  if (a->window < 0 || a->sinks < 0 || (a->window == 0 && a->sinks != 0) || !std::isfinite(a->softmax_scale)) return QKV_ERR_SHAPE;
+  if (misaligned(a->q_dev, 16) || misaligned(a->out_dev, 16) || misaligned(a->lse_dev, 4) || misaligned(a->status_dev, 4)) return QKV_ERR_ALIGN;
+  return QKV_OK;
+}
+
+// Tiles of 32 tokens that the longest sequence the table has room for can have, sinks and the window's edge included.
+uint64_t most_tiles(const qkv_pages_t* p) { return ((uint64_t)p->row_pages * (uint64_t)p->page_tokens + 31u) / 32u + 2u; }
+
+// A window that holds any sequence the table has room for is none.
+uint32_t window_of(const qkv_pages_t* p, int32_t window) { return (int64_t)window >= (int64_t)p->row_pages * p->page_tokens ? 0u : (uint32_t)window; }
+
+struct AttendPlan {
+  uint32_t rep, blocks, heads;      // query heads per kv head, groups of 16, heads of a group
+  uint64_t items;
+  uint32_t most;                    // shares
+  bool split;
+  uint64_t floats;
+};
+int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
+  a.rep = (uint32_t)(q_heads / p->kv_heads);
+  a.blocks = (a.rep + 15u) / 16u;
+  a.heads = a.rep < 16u ? a.rep : 16u;
+  a.items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
+  if (a.items * most_tiles(p) >= (1ull << 31)) return QKV_ERR_SHAPE;
+  a.split = most_tiles(p) - 2u > kAttendLeast;
+  const uint64_t shares = (a.items * most_tiles(p) + kAttendLeast - 1u) / kAttendLeast;
+  a.most = (uint32_t)(shares < kAttendShares ? shares : kAttendShares);
+  a.floats = a.split ? (a.items + a.most) * a.heads * ((uint64_t)p->head_dim + 2u) : 0u;
+  return QKV_OK;
+}
+
+struct PromptPlan {
+  uint32_t rep, per, splits;
+  uint64_t floats;
+};
+int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
+  if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
+  a.rep = (uint32_t)(q_heads / p->kv_heads);
+  a.per = kPromptRows / a.rep;
+  const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
+  if (tiles >= (1ull << 31)) return QKV_ERR_SHAPE;
+  // Few query tiles: the keys are split until there are about two workgroups a CU, into shares of at least 256 tokens.
+  const uint64_t room = ((uint64_t)p->row_pages * (uint64_t)p->page_tokens + 255u) / 256u;
+  uint64_t n = kPromptTarget / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
+  if (n > room) n = room;
+  if (n > 64u) n = 64u;
+  a.splits = n < 2u ? 1u : (uint32_t)n;
+  a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
+  return QKV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int qkv_pages_append(const qkv_pages_t* pages, const qkv_rows_t* rows, uint32_t* status_dev, void* stream) {
+  const int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!rows || !rows->k_dev || !rows->v_dev) return QKV_ERR_NULL;
+  if (rows->layer_begin < 0 || rows->layer_count < 1 || rows->layer_begin > pages->layers - rows->layer_count) return QKV_ERR_SHAPE;
+  if (rows->tokens < 0 || rows->tokens >= (1ll << 31) || (!rows->starts_dev && rows->tokens != pages->rows)) return QKV_ERR_SHAPE;
+  const int64_t strides[3] = {rows->layer_stride, rows->head_stride, rows->token_stride};
+  for (int i = 0; i < 3; ++i)
+    if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 40)) return QKV_ERR_SHAPE;
+  if (misaligned(rows->k_dev, 16) || misaligned(rows->v_dev, 16) || misaligned(rows->starts_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  AppendArgs a;
+  a.k = static_cast<const uint8_t*>(rows->k_dev);
+  a.v = static_cast<const uint8_t*>(rows->v_dev);
+  a.layer_stride = (uint64_t)rows->layer_stride * 2u;
+  a.head_stride = (uint64_t)rows->head_stride * 2u;
+  a.token_stride = (uint64_t)rows->token_stride * 2u;
+  a.starts = rows->starts_dev;
+  a.tokens = (uint32_t)rows->tokens;
+  a.layer_begin = (uint32_t)rows->layer_begin;
+  a.layer_count = (uint32_t)rows->layer_count;
+  a.status = status_dev;
+  return launch_pages_append(cache_of(pages), a, static_cast<hipStream_t>(stream)) == hipSuccess ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_reserve(const qkv_pages_t* pages, const int32_t* more_dev, uint32_t* status_dev, void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc) return rc;
+  if (!status_dev) return QKV_ERR_NULL;
+  if (misaligned(more_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  return launch_pages_reserve(cache_of(pages), more_dev, status_dev, static_cast<hipStream_t>(stream)) == hipSuccess ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_fork(const qkv_pages_t* pages, const int32_t* source_dev, const int32_t* target_dev, int32_t count, uint32_t* status_dev,
+                   void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc) return rc;
+  if (!source_dev || !target_dev || !status_dev) return QKV_ERR_NULL;
+  if (count < 1 || count > pages->rows) return QKV_ERR_SHAPE;
+  if (misaligned(source_dev, 4) || misaligned(target_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  return launch_pages_fork(cache_of(pages), source_dev, target_dev, (uint32_t)count, status_dev, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_free(const qkv_pages_t* pages, const int32_t* rows_dev, int32_t count, int32_t window, int32_t sinks, uint32_t* status_dev,
+                   void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc) return rc;
+  if (count < 1 || count > pages->rows || (!rows_dev && count != pages->rows)) return QKV_ERR_SHAPE;
+  if (window < 0 || sinks < 0 || (window == 0 && sinks != 0)) return QKV_ERR_SHAPE;
+  if (misaligned(rows_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  return launch_pages_free(cache_of(pages), rows_dev, (uint32_t)count, (uint32_t)window, (uint32_t)sinks, status_dev,
+                           static_cast<hipStream_t>(stream)) == hipSuccess ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_compact_workspace(const qkv_pages_t* pages, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  const int rc = check_pages(pages, false);
+  if (rc) return rc;
+  *bytes_out = 16u + 12u * (uint64_t)pages->pages;
+  return QKV_OK;
+}
+
+int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspace_dev, uint64_t workspace_bytes, uint32_t* status_dev,
+                      void* stream) {
+  const int rc = check_pages(pages, true);
+  if (rc) return rc;
+  if (!workspace_dev || !status_dev) return QKV_ERR_NULL;
+  uint64_t bytes = 0;
+  qkv_pages_compact_workspace(pages, &bytes);
+  if (workspace_bytes < bytes) return QKV_ERR_CAPACITY;
+  if (misaligned(workspace_dev, 16) || misaligned(live_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  return launch_pages_compact(cache_of(pages), live_dev, static_cast<int32_t*>(workspace_dev), status_dev, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_paged_attend_workspace(const qkv_pages_t* pages, int32_t q_heads, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_heads(pages, q_heads);
+  if (rc) return rc;
+  AttendPlan plan;
+  rc = plan_attend(pages, q_heads, plan);
+  if (rc) return rc;
+  *bytes_out = plan.floats * sizeof(float);
+  return QKV_OK;
+}
+
+int qkv_paged_attend(const qkv_pages_t* pages, const qkv_paged_query_t* query, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!query) return QKV_ERR_NULL;
+  rc = check_where(pages, query);
+  if (rc) return rc;
+  if (query->tokens != pages->rows || query->starts_dev) return QKV_ERR_SHAPE;
+  if ((query->prior_out_dev == nullptr) != (query->prior_lse_dev == nullptr)) return QKV_ERR_NULL;
+  AttendPlan plan;
+  rc = plan_attend(pages, query->q_heads, plan);
+  if (rc) return rc;
+  if (plan.floats != 0u && !query->workspace_dev) return QKV_ERR_NULL;
+  if (query->workspace_bytes < plan.floats * sizeof(float)) return QKV_ERR_CAPACITY;
+  if (misaligned(query->workspace_dev, 16) || misaligned(query->prior_out_dev, 16) || misaligned(query->prior_lse_dev, 4)) return QKV_ERR_ALIGN;
+  PagedAttendArgs a;
+  a.p = layer_of(pages, query->layer);
+  a.q = static_cast<const uint8_t*>(query->q_dev);
+  a.q_token_stride = (uint64_t)query->q_token_stride * 2u;
+  a.q_head_stride = (uint64_t)query->q_head_stride * 2u;
+  a.rep = plan.rep;
+  a.blocks = plan.blocks;
+  a.window = window_of(pages, query->window);
+  a.sinks = a.window ? (uint32_t)query->sinks : 0u;
+  a.scale_log2 = (float)((double)query->softmax_scale * 1.4426950408889634);
+  a.prior_out = query->prior_out_dev;
+  a.prior_lse = query->prior_lse_dev;
+  a.out = static_cast<float*>(query->out_dev);
+  a.lse = query->lse_dev;
+  a.part_o = static_cast<float*>(query->workspace_dev);
+  a.part_ml = plan.floats ? a.part_o + (plan.items + plan.most) * plan.heads * (uint64_t)pages->head_dim : nullptr;
+  a.most = plan.most;
+  a.status = query->status_dev;
+  return launch_paged_attend(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, plan.split, static_cast<hipStream_t>(stream)) ==
+                 hipSuccess ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_paged_prompt_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_t tokens, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_heads(pages, q_heads);
+  if (rc) return rc;
+  PromptPlan plan;
+  rc = plan_prompt(pages, q_heads, tokens, plan);
+  if (rc) return rc;
+  *bytes_out = plan.floats * sizeof(float);
+  return QKV_OK;
+}
+
+int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!query || !query->starts_dev) return QKV_ERR_NULL;
+  rc = check_where(pages, query);
+  if (rc) return rc;
+  if (query->prior_out_dev || query->prior_lse_dev) return QKV_ERR_SHAPE;
+  PromptPlan plan;
+  rc = plan_prompt(pages, query->q_heads, query->tokens, plan);
+  if (rc) return rc;
+  if (plan.floats != 0u && !query->workspace_dev) return QKV_ERR_NULL;
+  if (query->workspace_bytes < plan.floats * sizeof(float)) return QKV_ERR_CAPACITY;
+  if (misaligned(query->workspace_dev, 16) || misaligned(query->starts_dev, 4)) return QKV_ERR_ALIGN;
+  PagedPromptArgs a;
+  a.p = layer_of(pages, query->layer);
+  a.q = static_cast<const uint8_t*>(query->q_dev);
+  a.q_token_stride = (uint64_t)query->q_token_stride * 2u;
+  a.q_head_stride = (uint64_t)query->q_head_stride * 2u;
+  a.starts = query->starts_dev;
+  a.tokens = (uint32_t)query->tokens;
+  a.rep = plan.rep;
+  a.per = plan.per;
+  a.window = window_of(pages, query->window);
+  a.sinks = a.window ? (uint32_t)query->sinks : 0u;
+  a.scale_log2 = (float)(std::fabs((double)query->softmax_scale) * 1.4426950408889634);
+  if (!(a.scale_log2 >= 1e-37f)) a.scale_log2 = 1e-37f;        // 0: all scores equal, and -inf stays -inf
+  a.flip = query->softmax_scale < 0.0f ? 1u : 0u;
+  a.out = static_cast<uint8_t*>(query->out_dev);
+  a.lse = query->lse_dev;
+  a.part_o = static_cast<float*>(query->workspace_dev);
+  a.part_ml = plan.floats ? a.part_o + plan.splits * (uint64_t)query->tokens * (uint64_t)query->q_heads * (uint64_t)pages->head_dim : nullptr;
+  a.splits = plan.splits;
+  a.status = query->status_dev;
+  return launch_paged_prompt(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+}  // extern "C"

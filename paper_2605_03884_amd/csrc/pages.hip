@@ -1,0 +1,402 @@
+// pages.hip — a cache in pages: rows of new tokens written, and pages reserved, shared, given back and moved together.
+//
+// A page holds page_tokens tokens of every layer, kv head, K and V; refs[page] is how many sequences hold it, 0 (or less) is free.
+// All bookkeeping runs on the device, on whole numbers whose result does not hang on the order of the threads: pages are
+// given out lowest first, in the order of the rows.  What decides (reserve, the allocation of a fork, the plan of a
+// compaction) is one workgroup; what moves bytes is spread over the chip.
+#include <algorithm>
+
+#include "paged.h"
+#include "qkv_common.h"
+
+namespace qkv {
+namespace {
+
+constexpr uint32_t kPlanThreads = 1024;
+constexpr uint32_t kPicked = 4096;          // free pages a plan looks up at a time
+
+// ---------------------------------------------------------------- rows of new tokens
+//
+// A workgroup takes `block` tokens of one layer, of the keys or the values.  Its waves look up where the tokens go (row of the batch,
+// place in the sequence, page), then all threads copy 16 bytes at a time.  HEADS_FIRST: the new rows of a head lie together (a dense cache), so
+// consecutive threads take consecutive tokens of a head; otherwise the heads of a token.
+constexpr uint32_t kAppendThreads = 256;
+constexpr uint32_t kAppendBlock = 16;
+
+template <bool HEADS_FIRST>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(PageCache c, AppendArgs a, uint32_t block) {
+  __shared__ uint64_t to[kAppendBlock];                    // byte offset of the token's row in head 0, or ~0
+  const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
+  const uint32_t first = blockIdx.x * block, count = min(block, a.tokens - first);
+  const bool values = (blockIdx.y & 1u) != 0u;
+  const uint32_t layer = blockIdx.y >> 1;
+  for (uint32_t i = wave; i < count; i += kAppendThreads / kWaveSize) {
+    const uint32_t at = first + i;
+    uint64_t where = ~0ull;
+    uint32_t row = at, start = at, end = at + 1u;
+    if (a.starts) {
+      row = find_row(c.rows, lane, [&](uint32_t b) { return (uint32_t)a.starts[b] <= at; });
+      start = (uint32_t)a.starts[row];
+      end = (uint32_t)a.starts[row + 1u];
+    }
+    if (at >= start && at < end) {                         // a token behind the last row belongs to none
+      const int64_t place = (int64_t)c.lens[row] - (int64_t)(end - start) + (int64_t)(at - start);
+      const bool inside = place >= 0 && (uint64_t)place < ((uint64_t)c.row_pages << c.page_shift);
+      if (inside) {
+        const uint32_t page = (uint32_t)c.table[(uint64_t)row * c.row_pages + ((uint32_t)place >> c.page_shift)];
+        if (page < c.pages) where = (uint64_t)page * c.page_stride + ((uint32_t)place & ((1u << c.page_shift) - 1u)) * c.token_stride;
+        else if (lane == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
+      } else if (lane == 0u && (a.starts || c.lens[row] > 0)) {
+        flag(a.status, QKV_STATUS_BAD_ROW);
+      }
+    }
+    if (lane == 0u) to[i] = where;
+  }
+  __syncthreads();
+  const uint32_t chunks = c.head_dim / 8u, chunk_shift = (uint32_t)__builtin_ctz(c.head_dim) - 3u;
+  const uint8_t* from = (values ? a.v : a.k) + (uint64_t)layer * a.layer_stride;
+  uint8_t* pool = values ? c.v[a.layer_begin + layer] : c.k[a.layer_begin + layer];
+  const uint32_t all = (count * c.kv_heads) << chunk_shift;
+  for (uint32_t i = threadIdx.x; i < all; i += kAppendThreads) {
+    const uint32_t chunk = i & (chunks - 1u), rest = i >> chunk_shift;
+    const uint32_t head = HEADS_FIRST ? rest / count : rest % c.kv_heads, token = HEADS_FIRST ? rest % count : rest / c.kv_heads;
+    const uint64_t where = to[token];
+    if (where == ~0ull) continue;
+    const uint4 x = *reinterpret_cast<const uint4*>(from + (uint64_t)(first + token) * a.token_stride + head * a.head_stride + chunk * 16u);
+    *reinterpret_cast<uint4*>(pool + where + head * c.head_stride + chunk * 16u) = x;
+  }
+}
+
+// ---------------------------------------------------------------- bookkeeping
+
+// Exclusive prefix sum over the workgroup's threads; `total` is the sum.  `waves` is scratch of one word a wave.
+__device__ inline uint32_t block_scan(uint32_t x, uint32_t* waves, uint32_t& total) {
+  const uint32_t lane = threadIdx.x % kWaveSize, wave = threadIdx.x / kWaveSize;
+  const uint32_t sum = wave_inclusive_scan(x);
+  __syncthreads();                                        // the scratch may still be read
+  if (lane == kWaveSize - 1u) waves[wave] = sum;
+  __syncthreads();
+  uint32_t before = 0u;
+  total = 0u;
+#pragma unroll
+  for (uint32_t w = 0; w < kPlanThreads / kWaveSize; ++w) {
+    const uint32_t s = waves[w];
+    if (w < wave) before += s;
+    total += s;
+  }
+  return before + sum - x;
+}
+
+// Gives out pages: want(i) of them to item i < items, lowest free page first, in the items' order; give(i, j, page) takes the
+// j-th page of item i.  Nothing is given out unless all can be.  One workgroup; refs are changed by give().
+template <typename Want, typename Give>
+__device__ inline bool give_pages(const int32_t* refs, uint32_t pages, uint32_t items, uint32_t* picked, uint32_t* waves, Want want, Give give) {
+  uint32_t wanted = 0u, total;                             // fewer than rows * row_pages < 2^31 in all
+  for (uint32_t i = threadIdx.x; i < items; i += kPlanThreads) wanted += want(i);
+  block_scan(wanted, waves, total);
+  if (total == 0u) return true;
+  if (total > pages) return false;
+  uint32_t have = 0u;                                      // are there enough?
+  for (uint32_t base = 0; base < pages && have < total; base += 4u * kPlanThreads) {
+    uint32_t mine = 0u, sum;
+#pragma unroll
+    for (uint32_t k = 0; k < 4u; ++k) {
+      const uint32_t at = base + k * kPlanThreads + threadIdx.x;
+      mine += at < pages && refs[at] <= 0 ? 1u : 0u;
+    }
+    block_scan(mine, waves, sum);
+    have += sum;
+  }
+  if (have < total) return false;
+  uint32_t cursor = 0u;                                    // pages below it have been looked at
+  for (uint32_t done = 0u; done < total; done += kPicked) {
+    const uint32_t now = min(kPicked, total - done);
+    uint32_t found = 0u;
+    while (found < now) {                                  // there are enough, so this ends before the last page
+      const uint32_t at = cursor + threadIdx.x;
+      const bool is_free = at < pages && refs[at] <= 0;
+      uint32_t sum;
+      const uint32_t rank = found + block_scan(is_free ? 1u : 0u, waves, sum);
+      if (is_free && rank < now) picked[rank] = at;
+      if (found + sum >= now) {                            // the next round goes on behind the last one taken
+        __syncthreads();
+        cursor = picked[now - 1u] + 1u;
+      } else {
+        cursor += kPlanThreads;
+      }
+      found += sum;
+    }
+    __syncthreads();
+    uint32_t before = 0u;
+    for (uint32_t base = 0; base < items; base += kPlanThreads) {
+      const uint32_t i = base + threadIdx.x, w = i < items ? want(i) : 0u;
+      uint32_t sum;
+      const uint32_t from = before + block_scan(w, waves, sum);
+      const uint32_t lo = max(from, done), hi = min(from + w, done + now);
+      for (uint32_t r = lo; r < hi; ++r) give(i, r - from, picked[r - done]);
+      before += sum;
+    }
+    __syncthreads();
+  }
+  return true;
+}
+
+__device__ inline uint32_t pages_for(uint32_t tokens, uint32_t shift) { return (uint32_t)(((uint64_t)tokens + (1u << shift) - 1u) >> shift); }
+
+__global__ __launch_bounds__(kPlanThreads) void reserve_kernel(PageCache c, const int32_t* more, uint32_t* status) {
+  __shared__ uint32_t picked[kPicked], waves[kPlanThreads / kWaveSize];
+  __shared__ uint32_t bad;
+  if (threadIdx.x == 0u) bad = 0u;
+  __syncthreads();
+  const uint64_t most = (uint64_t)c.row_pages << c.page_shift;
+  for (uint32_t i = threadIdx.x; i < c.rows; i += kPlanThreads) {
+    const int32_t len = c.lens[i], add = more ? more[i] : 1;
+    if (len < 0 || add < 0 || (uint64_t)len + (uint64_t)add > most) bad = 1u;
+  }
+  __syncthreads();
+  uint32_t verdict = bad ? QKV_STATUS_BAD_ROW : 0u;
+  if (!bad) {
+    const auto want = [&](uint32_t i) {
+      const uint32_t len = (uint32_t)c.lens[i], add = (uint32_t)(more ? more[i] : 1);
+      return pages_for(len + add, c.page_shift) - pages_for(len, c.page_shift);
+    };
+    const auto give = [&](uint32_t i, uint32_t j, uint32_t page) {
+      c.table[(uint64_t)i * c.row_pages + pages_for((uint32_t)c.lens[i], c.page_shift) + j] = (int32_t)page;
+      c.refs[page] = 1;
+    };
+    if (give_pages(c.refs, c.pages, c.rows, picked, waves, want, give)) {
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < c.rows; i += kPlanThreads) c.lens[i] += more ? more[i] : 1;
+    } else {
+      verdict = QKV_STATUS_NO_PAGES;
+    }
+  }
+  if (threadIdx.x == 0u) *status = verdict;
+}
+
+// Whether the pairs of a fork are what they may be: rows of the table, targets all different and none of them a source.  Every workgroup
+// that has to know looks for itself; `marks` has a bit for each row.
+__device__ inline bool pairs_fit(const int32_t* source, const int32_t* target, uint32_t n, uint32_t rows, uint32_t* marks, uint32_t* bad) {
+  for (uint32_t i = threadIdx.x; i < (rows + 31u) / 32u; i += blockDim.x) marks[i] = 0u;
+  if (threadIdx.x == 0u) *bad = 0u;
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+    const uint32_t s = (uint32_t)source[i], t = (uint32_t)target[i];
+    if (s >= rows || t >= rows) *bad = 1u;
+    else if (atomicOr(&marks[t / 32u], 1u << (t % 32u)) >> (t % 32u) & 1u) *bad = 1u;
+  }
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += blockDim.x) {
+    const uint32_t s = (uint32_t)source[i];
+    if (s < rows && (marks[s / 32u] >> (s % 32u) & 1u)) *bad = 1u;
+  }
+  __syncthreads();
+  return *bad == 0u;
+}
+
+// Adds `by` to the counts of the pages that row `row` holds in its first `entries` entries.
+__device__ inline void count_row(const PageCache& c, uint32_t row, uint32_t entries, int32_t by) {
+  for (uint32_t j = threadIdx.x; j < entries; j += blockDim.x) {
+    const uint32_t page = (uint32_t)c.table[(uint64_t)row * c.row_pages + j];
+    if (page < c.pages) atomicAdd(&c.refs[page], by);
+  }
+}
+
+constexpr uint32_t kRowThreads = 256;
+
+// What the targets held is given back.
+__global__ __launch_bounds__(kRowThreads) void fork_release_kernel(PageCache c, const int32_t* source, const int32_t* target, uint32_t n) {
+  __shared__ uint32_t marks[kMaxRows / 32], bad;
+  if (!pairs_fit(source, target, n, c.rows, marks, &bad)) return;
+  const uint32_t row = (uint32_t)target[blockIdx.x];
+  count_row(c, row, pages_for(held(c.lens[row], c.row_pages, c.page_shift), c.page_shift), -1);
+}
+
+// New pages for last pages that are not full; the targets' lengths.
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(PageCache c, const int32_t* source, const int32_t* target, uint32_t n, uint32_t* status) {
+  __shared__ uint32_t marks[kMaxRows / 32], bad;
+  __shared__ uint32_t picked[kPicked], waves[kPlanThreads / kWaveSize];
+  const bool fits = pairs_fit(source, target, n, c.rows, marks, &bad);
+  uint32_t verdict = fits ? 0u : QKV_STATUS_BAD_ROW;
+  if (fits) {
+    const auto length = [&](uint32_t i) { return held(c.lens[source[i]], c.row_pages, c.page_shift); };
+    const auto want = [&](uint32_t i) { return (length(i) & ((1u << c.page_shift) - 1u)) != 0u ? 1u : 0u; };
+    const auto give = [&](uint32_t i, uint32_t, uint32_t page) {
+      c.table[(uint64_t)(uint32_t)target[i] * c.row_pages + (length(i) >> c.page_shift)] = (int32_t)page;
+      c.refs[page] = 1;
+    };
+    if (give_pages(c.refs, c.pages, n, picked, waves, want, give)) {
+      for (uint32_t i = threadIdx.x; i < n; i += kPlanThreads) c.lens[target[i]] = (int32_t)length(i);
+    } else {
+      verdict = QKV_STATUS_NO_PAGES;
+    }
+  }
+  if (threadIdx.x == 0u) *status = verdict;
+}
+
+// Copies `tokens` tokens of all heads of page `from` to page `to`: threads `thread`, thread + threads, ... of 16 bytes each.
+__device__ inline void copy_tokens(const PageCache& c, uint8_t* pool, uint32_t from, uint32_t to, uint32_t tokens, uint32_t thread, uint32_t threads) {
+  const uint32_t chunk_shift = (uint32_t)__builtin_ctz(c.head_dim) - 3u, chunks = 1u << chunk_shift;
+  const uint8_t* a = pool + (uint64_t)from * c.page_stride;
+  uint8_t* b = pool + (uint64_t)to * c.page_stride;
+  const uint32_t all = (tokens * c.kv_heads) << chunk_shift;
+  for (uint32_t i = thread; i < all; i += threads) {
+    const uint32_t chunk = i & (chunks - 1u), rest = i >> chunk_shift, token = rest % tokens, head = rest / tokens;
+    const uint64_t at = head * c.head_stride + token * c.token_stride + chunk * 16u;
+    *reinterpret_cast<uint4*>(b + at) = *reinterpret_cast<const uint4*>(a + at);
+  }
+}
+
+// Pair blockIdx.x.  blockIdx.y = 0: shared pages go into the target's row and are counted, or, where there were no pages, the target
+// holds again what it held.  blockIdx.y = 1 + 2 * layer + (0: keys, 1: values): the tokens of the last page.
+__global__ __launch_bounds__(kRowThreads) void fork_fill_kernel(PageCache c, const int32_t* source, const int32_t* target, uint32_t* status) {
+  const uint32_t verdict = *status;
+  if (verdict & QKV_STATUS_BAD_ROW) return;
+  const uint32_t from = (uint32_t)source[blockIdx.x], to = (uint32_t)target[blockIdx.x];
+  const uint32_t length = held(c.lens[to], c.row_pages, c.page_shift), full = length >> c.page_shift, part = length & ((1u << c.page_shift) - 1u);
+  if (verdict & QKV_STATUS_NO_PAGES) {
+    if (blockIdx.y == 0u) count_row(c, to, pages_for(length, c.page_shift), 1);
+    return;
+  }
+  if (blockIdx.y == 0u) {
+    for (uint32_t j = threadIdx.x; j < full; j += kRowThreads) {
+      const int32_t page = c.table[(uint64_t)from * c.row_pages + j];
+      c.table[(uint64_t)to * c.row_pages + j] = page;
+      if ((uint32_t)page < c.pages) atomicAdd(&c.refs[page], 1);
+    }
+  } else if (part != 0u) {
+    const uint32_t at = (uint32_t)c.table[(uint64_t)from * c.row_pages + full], page = (uint32_t)c.table[(uint64_t)to * c.row_pages + full];
+    if (at >= c.pages) {
+      if (threadIdx.x == 0u) flag(status, QKV_STATUS_BAD_PAGE);
+      return;
+    }
+    const uint32_t layer = (blockIdx.y - 1u) >> 1;
+    copy_tokens(c, (blockIdx.y & 1u) != 0u ? c.k[layer] : c.v[layer], at, page, part, threadIdx.x, kRowThreads);
+  }
+}
+
+// Row rows[blockIdx.x] (or row blockIdx.x) gives its pages back: all of them, or those that no query at its last position or later sees.
+// An entry changes hands by an exchange, so a row that is listed twice gives each page back once.
+__global__ __launch_bounds__(kRowThreads) void free_kernel(PageCache c, const int32_t* rows, uint32_t window, uint32_t sinks, uint32_t* status) {
+  const uint32_t row = rows ? (uint32_t)rows[blockIdx.x] : blockIdx.x;
+  if (row >= c.rows) {
+    if (threadIdx.x == 0u) flag(status, QKV_STATUS_BAD_ROW);
+    return;
+  }
+  const uint32_t length = held(c.lens[row], c.row_pages, c.page_shift);
+  uint32_t first = 0u, end = pages_for(length, c.page_shift);
+  if (window != 0u) {
+    first = pages_for(sinks, c.page_shift);
+    end = length > window ? (length - window) >> c.page_shift : 0u;
+  }
+  for (uint32_t j = first + threadIdx.x; j < end; j += kRowThreads) {
+    const uint32_t page = (uint32_t)atomicExch(&c.table[(uint64_t)row * c.row_pages + j], -1);
+    if (page < c.pages) atomicSub(&c.refs[page], 1);
+  }
+  __syncthreads();
+  if (window == 0u && threadIdx.x == 0u) c.lens[row] = 0;
+}
+
+// ---------------------------------------------------------------- compaction
+//
+// With n pages in use, the k-th page in use at n or above goes to the k-th free page below n: sources and destinations are
+// apart, so all moves may run at once.  A page's rank is how many pages in use lie below it; `kept` pages in use lie below n, so the
+// movers have the ranks kept .. n - 1.  Workspace: {moves, n, kept, -}, the holes, the movers by rank, the ranks by page.
+__global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageCache c, int32_t* live_out, int32_t* work, uint32_t* status) {
+  __shared__ uint32_t waves[kPlanThreads / kWaveSize];
+  uint32_t mine = 0u, live;
+  for (uint32_t at = threadIdx.x; at < c.pages; at += kPlanThreads) mine += c.refs[at] > 0 ? 1u : 0u;
+  block_scan(mine, waves, live);
+  int32_t *holes = work + 4, *movers = holes + c.pages, *ranks = movers + c.pages;
+  uint32_t before = 0u;                                    // pages in use before this round
+  for (uint32_t base = 0; base < c.pages; base += kPlanThreads) {
+    const uint32_t at = base + threadIdx.x;
+    const bool used = at < c.pages && c.refs[at] > 0;
+    uint32_t sum;
+    const uint32_t rank = before + block_scan(used ? 1u : 0u, waves, sum);        // pages in use below `at`
+    if (at < live && !used) holes[at - rank] = (int32_t)at;
+    if (at >= live && used) {
+      ranks[at] = (int32_t)rank;
+      movers[rank] = (int32_t)at;
+    }
+    before += sum;
+  }
+  uint32_t below = 0u, kept;
+  for (uint32_t at = threadIdx.x; at < live; at += kPlanThreads) below += c.refs[at] > 0 ? 1u : 0u;
+  block_scan(below, waves, kept);
+  const uint32_t moves = live - kept;
+  for (uint32_t k = threadIdx.x; k < moves; k += kPlanThreads) {
+    const int32_t from = movers[kept + k], to = holes[k];
+    c.refs[to] = c.refs[from];
+    c.refs[from] = 0;
+  }
+  if (threadIdx.x == 0u) {
+    work[0] = (int32_t)moves;
+    work[1] = (int32_t)live;
+    work[2] = (int32_t)kept;
+    if (live_out) *live_out = (int32_t)live;
+    *status = 0u;
+  }
+}
+
+constexpr uint32_t kMoveBlocks = 2048;
+
+// Moves pages (a layer's keys or values of one move at a time) and renames them in the table.
+__global__ __launch_bounds__(kRowThreads) void compact_move_kernel(PageCache c, const int32_t* work) {
+  const uint32_t moves = (uint32_t)work[0], live = (uint32_t)work[1], kept = (uint32_t)work[2];
+  const int32_t *holes = work + 4, *movers = holes + c.pages, *ranks = movers + c.pages;
+  for (uint32_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
+    const uint32_t entries = pages_for(held(c.lens[row], c.row_pages, c.page_shift), c.page_shift);
+    for (uint32_t j = threadIdx.x; j < entries; j += kRowThreads) {
+      int32_t* entry = &c.table[(uint64_t)row * c.row_pages + j];
+      const uint32_t page = (uint32_t)*entry;
+      // a page that nobody counted is no page in use, whatever the entry says: it stays
+      if (page >= live && page < c.pages) {
+        const uint32_t k = (uint32_t)ranks[page] - kept;
+        if (k < moves && (uint32_t)movers[kept + k] == page) *entry = holes[k];
+      }
+    }
+  }
+  const uint64_t all = (uint64_t)moves * c.layers * 2u;
+  for (uint64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    const uint32_t k = (uint32_t)(i / (c.layers * 2u)), which = (uint32_t)(i % (c.layers * 2u));
+    copy_tokens(c, (which & 1u) != 0u ? c.v[which >> 1] : c.k[which >> 1], (uint32_t)movers[kept + k], (uint32_t)holes[k], 1u << c.page_shift, threadIdx.x,
+                kRowThreads);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_pages_append(const PageCache& c, const AppendArgs& a, hipStream_t stream) {
+  if (a.tokens == 0u) return hipSuccess;
+  const uint32_t block = (uint64_t)a.tokens * a.layer_count >= 8192u ? kAppendBlock : 4u;
+  const dim3 grid((a.tokens + block - 1u) / block, 2u * a.layer_count);
+  if (a.head_stride > a.token_stride) append_kernel<true><<<grid, kAppendThreads, 0, stream>>>(c, a, block);
+  else append_kernel<false><<<grid, kAppendThreads, 0, stream>>>(c, a, block);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_reserve(const PageCache& c, const int32_t* more, uint32_t* status, hipStream_t stream) {
+  reserve_kernel<<<1, kPlanThreads, 0, stream>>>(c, more, status);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PageCache& c, const int32_t* source, const int32_t* target, uint32_t n, uint32_t* status, hipStream_t stream) {
+  fork_release_kernel<<<n, kRowThreads, 0, stream>>>(c, source, target, n);
+  fork_plan_kernel<<<1, kPlanThreads, 0, stream>>>(c, source, target, n, status);
+  fork_fill_kernel<<<dim3(n, 1u + 2u * c.layers), kRowThreads, 0, stream>>>(c, source, target, status);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_free(const PageCache& c, const int32_t* rows, uint32_t n, uint32_t window, uint32_t sinks, uint32_t* status, hipStream_t stream) {
+  free_kernel<<<n, kRowThreads, 0, stream>>>(c, rows, window, sinks, status);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PageCache& c, int32_t* live, int32_t* workspace, uint32_t* status, hipStream_t stream) {
+  compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(c, live, workspace, status);
+  compact_move_kernel<<<kMoveBlocks, kRowThreads, 0, stream>>>(c, workspace);
+  return hipGetLastError();
+}
+
+}  // namespace qkv

@@ -1,0 +1,185 @@
+"""Attention of single tokens over pages, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_03884_amd as qkv
+from oracle import paged_ref
+from paged_case import TYPES, Cache, check_attend
+
+pytestmark = pytest.mark.gpu
+
+LENGTHS = [0, 1, 31, 32, 33, 129, 500]
+
+
+def queries(rows, heads, dim, kind, seed=5):
+    """A part of a fused projection's result: rows of 3 heads more than it has."""
+    wide = torch.randn(rows, (heads + 3) * dim, generator=torch.Generator().manual_seed(seed)).to(TYPES[kind])
+    return wide, wide[:, dim: (heads + 1) * dim].view(rows, heads, dim)
+
+
+def expected(cache, q, scale, window=0, sinks=0, absent=None, layer=0):
+    parts = [paged_ref.attend(q[b:b + 1].double().numpy(), K, V, [cache.lens[b] - 1], scale, window, sinks, () if absent is None else absent[b])
+             for b, (K, V) in enumerate(cache.rows(layer))]
+    return [np.concatenate(x) for x in zip(*parts)]
+
+
+def run(cache, q_heads, dim, scale, layer=0, window=0, sinks=0, prior=None, with_lse=True, workspace=None, seed=5):
+    rows = len(cache.lens)
+    wide, q = queries(rows, q_heads, dim, cache.kind, seed)
+    gq = wide.cuda()[:, dim: (q_heads + 1) * dim].view(rows, q_heads, dim)
+    out = torch.full((rows, q_heads, dim), 7.0, device="cuda")
+    lse = torch.full((rows, q_heads), 7.0, device="cuda") if with_lse else None
+    qkv.paged_attend(cache.pages, gq, scale, out, lse, layer=layer, window=window, sinks=sinks, prior=prior, workspace=workspace, status=cache.status)
+    torch.cuda.synchronize()
+    return q, out.double().cpu().numpy(), None if lse is None else lse.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("q_heads,heads,dim", [(4, 4, 128), (8, 2, 128), (5, 1, 64), (14, 2, 64), (34, 2, 64), (20, 1, 128), (4, 2, 256)])
+def test_heads_and_types(kind, q_heads, heads, dim):
+    cache = Cache(LENGTHS, heads, dim, 16, kind, layers=2, seed=dim + q_heads)
+    q, out, lse = run(cache, q_heads, dim, dim ** -0.5, layer=1)
+    check_attend(out, lse, expected(cache, q, dim ** -0.5, layer=1), dim, 500)
+    assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("size", [1, 8, 16, 32, 64, 512])
+@pytest.mark.parametrize("layout", ["heads", "tokens", "both"])
+def test_page_sizes_and_layouts(size, layout):
+    cache = Cache([300, 0, 64, 7], 2, 128, size, layout=layout, seed=size)
+    q, out, lse = run(cache, 6, 128, 0.07)
+    check_attend(out, lse, expected(cache, q, 0.07), 128, 300)
+    assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (32, 0), (33, 4), (100, 32), (100, 45), (100, 1000), (499, 1), (500, 4), (5000, 4), (64, 0)])
+@pytest.mark.parametrize("size", [8, 64])
+def test_windows(window, sinks, size):
+    """Pages that are out of sight may be gone: their entries name nothing."""
+    cache = Cache(LENGTHS, 2, 64, size, "bf16" if window == 100 else "fp16", seed=window)
+    rows = cache.rows()
+    for b, n in enumerate(cache.lens):
+        for j in range(-(-n // size)):
+            if (j + 1) * size <= n - window and j * size >= sinks:
+                cache.gtable[b, j] = -1
+    q = queries(len(cache.lens), 6, 64, cache.kind)[1]
+    want = expected(cache, q, 0.125, window, sinks)
+    q, out, lse = run(cache, 6, 64, 0.125, window=window, sinks=sinks)
+    check_attend(out, lse, want, 64, 500)
+    assert int(cache.status) == 0 and len(rows) == len(LENGTHS)
+
+
+@pytest.mark.parametrize("lens,heads,q_heads", [([4097], 1, 2), ([9000, 3, 1200], 2, 8), ([1] * 130 + [3000], 1, 1)])
+def test_long_and_many_rows(lens, heads, q_heads):
+    cache = Cache(lens, heads, 64, 16, seed=len(lens))
+    q, out, lse = run(cache, q_heads, 64, 0.2)
+    check_attend(out, lse, expected(cache, q, 0.2), 64, max(lens))
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-20, 40.0])
+def test_scales(scale):
+    cache = Cache([200, 33], 1, 64, 16, seed=3)
+    q, out, lse = run(cache, 4, 64, scale)
+    check_attend(out, lse, expected(cache, q, float(np.float32(scale))), 64, 200)
+
+
+def test_without_lse_and_with_a_larger_workspace():
+    cache = Cache(LENGTHS, 2, 128, 16, seed=9)
+    q, a, lse = run(cache, 8, 128, 0.1)
+    _, b, none = run(cache, 8, 128, 0.1, with_lse=False, workspace=torch.full((1 << 22,), 255, dtype=torch.uint8, device="cuda"))
+    assert none is None and np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("size", [16, 64])
+def test_entries_that_name_no_page(size):
+    """Their tokens are not seen, and the status word says so."""
+    cache = Cache([200, 90, 40], 2, 64, size, seed=1)
+    absent = [set(), set(), set()]
+    for b, j, page in ((0, 1, -1), (0, 2, cache.k.shape[1]), (2, 0, 0x7FFFFFFF)):
+        cache.gtable[b, j] = page
+        absent[b] |= set(range(j * size, (j + 1) * size))
+    q = queries(3, 4, 64, "fp16")[1]
+    want = expected(cache, q, 0.125, absent=absent)
+    q, out, lse = run(cache, 4, 64, 0.125)
+    check_attend(out, lse, want, 64, 200)
+    assert int(cache.status) == qkv.STATUS_BAD_PAGE
+
+
+def test_lengths_that_the_table_has_no_room_for():
+    """They count as what there is room for; negative ones as none."""
+    cache = Cache([160, 32], 1, 64, 16, extra_entries=0, seed=2)
+    cache.glens.copy_(torch.tensor([100000, -3], dtype=torch.int32))
+    q, out, lse = run(cache, 2, 64, 0.125)
+    cache.lens = [160, 0]
+    check_attend(out, lse, expected(cache, q, 0.125), 64, 160)
+
+
+def test_infinite_and_missing_numbers_in_what_is_seen():
+    """A value that is infinite or no number makes its own dimension so, a score of -inf weighs nothing."""
+    cache = Cache([70], 1, 64, 16, seed=4)
+    page = int(cache.table[0, 1])
+    cache.v[0, page, 0, 3, 5] = float("inf")
+    cache.v[0, page, 0, 4, 9] = float("nan")
+    cache.k[0, page, 0, 6] = 0.0
+    cache.gpu()
+    q, out, lse = run(cache, 2, 64, 0.125)
+    K, V = cache.rows()[0]
+    clean = V.copy()
+    clean[:, :, [5, 9]] = 0.0
+    want = [np.asarray(x) for x in paged_ref.attend(q.double().numpy(), K, clean, [69], 0.125)]
+    assert np.isposinf(out[..., 5]).all() and np.isnan(out[..., 9]).all()
+    out[..., [5, 9]] = 0.0
+    check_attend(out, lse, want, 64, 70)
+
+
+@pytest.mark.parametrize("lens", [[0, 5, 300], [0, 1500, 40]])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_joined_with_attention_over_other_tokens(lens, in_place):
+    cache = Cache(lens, 2, 128, 16, seed=6)
+    gen = torch.Generator().manual_seed(8)
+    other, other_lse = torch.randn(3, 8, 128, generator=gen), torch.randn(3, 8, generator=gen) * 3 + 4
+    other_lse[:, 1], other_lse[:, 2] = -float("inf"), 80.0
+    wide, q = queries(3, 8, 128, "fp16")
+    alone = expected(cache, q, 0.1)
+    out, lse = paged_ref.joined(alone[0], alone[1], other.double().numpy(), other_lse.double().numpy())
+    go, gl = other.cuda(), other_lse.cuda()
+    o, l = (go, gl) if in_place else (torch.empty_like(go), torch.empty_like(gl))
+    qkv.paged_attend(cache.pages, q.cuda(), 0.1, o, l, prior=(go, gl))
+    # joining weighs two results with factors that are off by a few steps, and by lse's own error in the exponent
+    s = (alone[3] * 128 * 2.0 ** -24 + alone[4] * 6 * 2.0 ** -24 + 2.0 ** -22 + 4 * 2.0 ** -24 * (np.abs(np.where(np.isfinite(lse), lse, 0)) + 80))[..., None]
+    size = alone[2] + np.abs(other.double().numpy())
+    assert (np.abs(o.double().cpu().numpy() - out) <= (4 * s + (max(lens) + 64) * 2.0 ** -24) * size).all()
+    some = np.isfinite(lse)
+    assert (np.abs(l.double().cpu().numpy()[some] - lse[some]) <= (s[..., 0] + max(lens) * 2.0 ** -24 + 2.0 ** -21)[some]).all()
+    assert np.array_equal(np.isneginf(l.cpu().numpy()), ~some)
+
+
+def test_the_same_call_gives_the_same_bits_and_other_streams_wait_for_nothing_of_it():
+    cache = Cache([900, 1, 333, 0], 2, 64, 16, seed=12)
+    _, a, la = run(cache, 8, 64, 0.125)
+    side = torch.cuda.Stream()
+    wide, q = queries(4, 8, 64, "fp16")
+    gq = q.cuda()
+    outs = [torch.empty(4, 8, 64, device="cuda") for _ in range(2)]
+    spaces = [torch.empty(qkv.paged_attend_workspace(cache.pages, 8), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    qkv.paged_attend(cache.pages, gq, 0.125, outs[0], workspace=spaces[0])
+    with torch.cuda.stream(side):
+        qkv.paged_attend(cache.pages, gq, 0.125, outs[1], workspace=spaces[1])
+    torch.cuda.synchronize()
+    assert np.array_equal(outs[0].double().cpu().numpy(), a) and np.array_equal(outs[1].double().cpu().numpy(), a)
+
+
+def test_tensors_that_are_refused():
+    cache = Cache([40], 2, 64, 16)
+    q, out = torch.zeros(1, 4, 64, dtype=torch.float16, device="cuda"), torch.zeros(1, 4, 64, device="cuda")
+    for bad in (dict(q=q.float()), dict(q=q.transpose(1, 2)), dict(q=q.cpu()), dict(q=q[:, :, :32]), dict(out=out.half()), dict(out=out[:, :2]),
+                dict(lse=out[:, :, 0]), dict(prior=(out, out)), dict(workspace=out), dict(status=torch.zeros(1, dtype=torch.int64, device="cuda"))):
+        with pytest.raises(ValueError):
+            a = {"q": q, "out": out, **bad}
+            qkv.paged_attend(cache.pages, a.pop("q"), 0.1, a.pop("out"), **a)
+    with pytest.raises(qkv.QkvError):
+        qkv.paged_attend(cache.pages, q, 0.1, out, layer=1)
+    with pytest.raises(qkv.QkvError):
+        qkv.paged_attend(cache.pages, q[:, :3], 0.1, out[:, :3].contiguous())

@@ -1,0 +1,170 @@
+"""Attention of many new tokens over pages, against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2605_03884_amd as qkv
+from oracle import paged_ref
+from paged_case import TYPES, Cache, check_prompt
+
+pytestmark = pytest.mark.gpu
+
+
+def run(cache, new, q_heads, dim, scale, layer=0, window=0, sinks=0, behind=3, seed=5, with_lse=True):
+    """`behind` tokens of the batch belong to no row."""
+    tokens = sum(new) + behind
+    starts = torch.tensor([sum(new[:i]) for i in range(len(new) + 1)], dtype=torch.int32)
+    wide = torch.randn(tokens, (q_heads + 2) * dim, generator=torch.Generator().manual_seed(seed)).to(TYPES[cache.kind])
+    cut = lambda x: x[:, dim: (q_heads + 1) * dim].view(tokens, q_heads, dim)  # noqa: E731
+    out = torch.full((tokens, q_heads, dim), 7.0, dtype=TYPES[cache.kind], device="cuda")
+    lse = torch.full((tokens, q_heads), 7.0, device="cuda") if with_lse else None
+    qkv.paged_prompt(cache.pages, cut(wide.cuda()), starts.cuda(), scale, out, lse, layer=layer, window=window, sinks=sinks, status=cache.status)
+    torch.cuda.synchronize()
+    out = out.double().cpu().numpy()
+    assert (out[tokens - behind:] == 7.0).all() and (lse is None or (lse[tokens - behind:] == 7.0).all())
+    return cut(wide)[: sum(new)], out[: sum(new)], None if lse is None else lse.double().cpu().numpy()[: sum(new)]
+
+
+def expected(cache, new, q, scale, window=0, sinks=0, absent=None, layer=0):
+    parts, at = [], 0
+    for b, (K, V) in enumerate(cache.rows(layer)):
+        n = cache.lens[b]
+        parts.append(paged_ref.attend(q[at:at + new[b]].double().numpy(), K, V, list(range(n - new[b], n)), scale, window, sinks, () if absent is None else absent[b]))
+        at += new[b]
+    return [np.concatenate(x) for x in zip(*parts)]
+
+
+def check(cache, new, got, want, dim):
+    q, out, lse = got
+    most = max([float(np.abs(V).max()) for _, V in cache.rows() if V.size] + [1.0])
+    check_prompt(out, lse, want, dim, max(cache.lens), cache.kind, most)
+
+
+NEW, OLD = [1, 0, 70, 33, 129], [0, 5, 0, 100, 64]
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("q_heads,heads,dim", [(4, 4, 128), (8, 2, 128), (5, 1, 64), (14, 2, 64), (34, 1, 64), (128, 1, 64), (4, 2, 256)])
+def test_heads_and_types(kind, q_heads, heads, dim):
+    new, old = ([1, 0, 9, 20], [0, 5, 0, 70]) if q_heads > 16 else (NEW, OLD)
+    cache = Cache([a + b for a, b in zip(new, old)], heads, dim, 16, kind, layers=2, seed=dim + q_heads)
+    got = run(cache, new, q_heads, dim, dim ** -0.5, layer=1)
+    check(cache, new, got, expected(cache, new, got[0], dim ** -0.5, layer=1), dim)
+    assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("size", [1, 8, 16, 32, 64, 256])
+@pytest.mark.parametrize("layout", ["heads", "tokens", "both"])
+def test_page_sizes_and_layouts(size, layout):
+    new, lens = [40, 100, 3], [40, 150, 64]
+    cache = Cache(lens, 2, 128, size, layout=layout, seed=size)
+    got = run(cache, new, 6, 128, 0.07)
+    check(cache, new, got, expected(cache, new, got[0], 0.07), 128)
+    assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (32, 0), (33, 4), (64, 64), (65, 70), (100, 1000), (130, 3), (5000, 4)])
+@pytest.mark.parametrize("size", [8, 64])
+def test_windows(window, sinks, size):
+    """Pages that no new token sees may be gone: their entries name nothing."""
+    new, old = [200, 1, 30], [150, 299, 320]
+    cache = Cache([a + b for a, b in zip(new, old)], 1, 64, size, "bf16" if window == 33 else "fp16", seed=window)
+    for b, n in enumerate(old):
+        for j in range(-(-cache.lens[b] // size)):
+            if (j + 1) * size <= n + 1 - window and j * size >= sinks:
+                cache.gtable[b, j] = -1
+    got = run(cache, new, 3, 64, 0.125, window=window, sinks=sinks)
+    check(cache, new, got, expected(cache, new, got[0], 0.125, window, sinks), 64)
+    assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("new,old,window", [([5], [3000], 0), ([1], [5000], 0), ([20, 3], [2500, 0], 0), ([17], [4000], 900), ([0, 2, 0], [10, 2100, 0], 0)])
+def test_few_queries_behind_many_keys(new, old, window):
+    cache = Cache([a + b for a, b in zip(new, old)], 1, 64, 16, seed=len(new) + window, extra_entries=4)
+    assert qkv.paged_prompt_workspace(cache.pages, 4, sum(new) + 3) > 0
+    got = run(cache, new, 4, 64, 0.125, window=window, sinks=2 if window else 0)
+    check(cache, new, got, expected(cache, new, got[0], 0.125, window, 2 if window else 0), 64)
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 3.0])
+def test_scales(scale):
+    cache = Cache([90, 33], 1, 64, 16, seed=3)
+    got = run(cache, [90, 10], 4, 64, scale)
+    check(cache, [90, 10], got, expected(cache, [90, 10], got[0], float(np.float32(scale))), 64)
+
+
+def test_scores_that_rise_from_key_to_key():
+    """The running maximum moves in every tile, by more and by less than what is put up with."""
+    cache = Cache([300], 1, 64, 16, seed=5, strong=1.0)
+    cache.k[:] = torch.where(torch.isnan(cache.k), cache.k, cache.k * 0.05)
+    for t in range(300):
+        cache.k[0, cache.table[0, t // 16], 0, t % 16, 0] = t * 0.5
+    cache.gpu()
+    got = run(cache, [300], 2, 64, 0.3, seed=7)
+    check(cache, [300], got, expected(cache, [300], got[0], float(np.float32(0.3))), 64)
+
+
+@pytest.mark.parametrize("size", [16, 128])
+def test_entries_that_name_no_page(size):
+    cache = Cache([200, 90], 1, 64, size, seed=1)
+    absent = [set(range(size, 2 * size)), set()]
+    cache.gtable[0, 1] = -1
+    got = run(cache, [60, 90], 4, 64, 0.125)
+    check(cache, [60, 90], got, expected(cache, [60, 90], got[0], 0.125, absent=absent), 64)
+    assert int(cache.status) == qkv.STATUS_BAD_PAGE
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+def test_infinite_and_missing_numbers_behind_a_query(kind):
+    """Values of later tokens do not touch the earlier ones, keys of theirs neither; a query that sees them has them in their own dimensions."""
+    cache = Cache([100], 1, 64, 16, kind, seed=4)
+    for t, d, x in ((50, 5, "inf"), (50, 6, "nan"), (77, 40, "-inf")):
+        cache.v[0, cache.table[0, t // 16], 0, t % 16, d] = float(x)
+    cache.gpu()
+    q, out, lse = run(cache, [100], 2, 64, 0.125)
+    K, V = cache.rows()[0]
+    want = [x.copy() for x in paged_ref.attend(q.double().numpy(), K, np.where(np.isfinite(V), V, 0.0), list(range(100)), 0.125)]
+    assert np.isposinf(out[50:, :, 5]).all() and np.isnan(out[50:, :, 6]).all() and np.isneginf(out[77:, :, 40]).all()
+    for t, d in ((50, 5), (50, 6), (77, 40)):
+        out[t:, :, d] = want[0][t:, :, d]
+    check_prompt(out, lse, want, 64, 100, kind, float(np.abs(V[np.isfinite(V)]).max()))
+
+
+def test_a_row_with_more_new_tokens_than_length():
+    """Tokens in front of the sequence see nothing; the status word says so."""
+    cache = Cache([10, 40], 1, 64, 16, seed=2)
+    q, out, lse = run(cache, [15, 40], 2, 64, 0.125)
+    assert int(cache.status) == qkv.STATUS_BAD_ROW
+    assert (out[:5] == 0).all() and np.isneginf(lse[:5]).all()
+    cache.lens = [10, 40]
+    want = expected(cache, [10, 40], q[5:], 0.125)
+    check_prompt(out[5:], lse[5:], want, 64, 40, "fp16", 20.0)
+
+
+def test_batches_that_make_no_sense_stay_inside():
+    cache = Cache([10, 40], 1, 64, 16, seed=2)
+    q, out = torch.zeros(20, 2, 64, dtype=torch.float16, device="cuda"), torch.zeros(20, 2, 64, dtype=torch.float16, device="cuda")
+    for starts in ([0, 500, 7], [-4, 3, 9], [30, 40, 50], [5, 2, 1]):
+        cache.status.zero_()
+        qkv.paged_prompt(cache.pages, q, torch.tensor(starts, dtype=torch.int32, device="cuda"), 0.125, out, status=cache.status)
+        assert int(cache.status) == qkv.STATUS_BAD_ROW, starts
+
+
+def test_without_lse_the_same_bits():
+    cache = Cache([200], 2, 128, 16, seed=9)
+    _, a, _ = run(cache, [150], 8, 128, 0.1)
+    _, b, none = run(cache, [150], 8, 128, 0.1, with_lse=False)
+    assert none is None and np.array_equal(a, b)
+
+
+def test_tensors_that_are_refused():
+    cache = Cache([40], 2, 64, 16)
+    q, starts = torch.zeros(6, 4, 64, dtype=torch.float16, device="cuda"), torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+    out = torch.zeros_like(q)
+    for bad in (dict(q=q.float()), dict(q=q.transpose(0, 2)), dict(out=out.float()), dict(out=out[:3]), dict(starts=starts.long()), dict(starts=starts[:1]),
+                dict(starts=starts.cpu()), dict(lse=out)):
+        with pytest.raises(ValueError):
+            a = {"q": q, "out": out, "starts": starts, **bad}
+            qkv.paged_prompt(cache.pages, a.pop("q"), a.pop("starts"), 0.1, a.pop("out"), **a)
+    with pytest.raises(qkv.QkvError):
+        qkv.paged_prompt(cache.pages, q[:0], starts, 0.1, out[:0])
