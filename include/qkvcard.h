@@ -506,8 +506,8 @@ int qkv_card_attend_static(const void* card_dev, uint64_t card_bytes, const qkv_
  * The pointer arrays are host memory, read before a call returns.
  *
  * Shapes: layers 1 .. 64; head_dim 64, 128, 256; page_tokens a power of two up to 2^20; pages < 2^31; rows <= 65536; row_pages * page_tokens
- * (room for one sequence) and rows * row_pages < 2^31; strides multiples of 8 elements below 2^31, token_stride >= head_dim; layer
- * pointers 16-byte aligned, others 4 (QKV_ERR_SHAPE, QKV_ERR_ALIGN).  The library cannot see the tensors' extents.
+ * (room for one sequence) and rows * row_pages < 2^31; strides multiples of 8 elements below 2^31, token_stride >= head_dim,
+ * page_tokens * token_stride <= 2^30; layer pointers 16-byte aligned, others 4 (QKV_ERR_SHAPE, QKV_ERR_ALIGN).  The library cannot see the tensors' extents.
  *
  * What only the device sees never makes a call leave these tensors: lengths count as 0 .. row_pages * page_tokens, an entry that names no
  * page is QKV_STATUS_BAD_PAGE.  Status words: qkv_pages_reserve, _fork and _compact need one and set it (0 when all is well); the

@@ -64,7 +64,7 @@ QKV_HD TileRange tile_range(const Seen& s, uint32_t i) {
   return t;
 }
 
-// `total` tiles dealt to `shares` in a row, the first ones one more than the last ones.
+// `total` tiles dealt to shares in a row, the first ones one more than the last ones.
 struct Shares {
   uint32_t shares, each, more;       // share i has each + (i < more) tiles
 };

@@ -7,7 +7,6 @@ using namespace qkv;
 
 namespace {
 
-constexpr uint32_t kAttendShares = 4096;      // shares of the decode kernel's work at most: waves that fit the chip at four a SIMD
 constexpr uint32_t kPromptRows = 128;         // (query token, query head) pairs of a prompt tile
 constexpr uint32_t kPromptTarget = 512;       // workgroups the prompt kernel's work is split into, where there are fewer query tiles
 
@@ -24,7 +23,7 @@ int check_pages(const qkv_pages_t* p, bool counted) {
   const int64_t strides[3] = {p->page_stride, p->head_stride, p->token_stride};
   for (int i = 0; i < 3; ++i)
     if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 31)) return QKV_ERR_SHAPE;
-  if (p->token_stride < p->head_dim) return QKV_ERR_SHAPE;
+  if (p->token_stride < p->head_dim || (int64_t)p->page_tokens * p->token_stride > (1ll << 30)) return QKV_ERR_SHAPE;
   if ((int64_t)p->page_tokens * p->kv_heads * p->head_dim >= (1ll << 31)) return QKV_ERR_SHAPE;     // a page's own size counts in 32 bits
   if (misaligned(p->table_dev, 4) || misaligned(p->lens_dev, 4) || misaligned(p->refs_dev, 4)) return QKV_ERR_ALIGN;
   for (int i = 0; i < p->layers; ++i) {
@@ -113,8 +112,10 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
   a.items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
   if (a.items * most_tiles(p) >= (1ull << 31)) return QKV_ERR_SHAPE;
   a.split = most_tiles(p) - 2u > kAttendLeast;
-  const uint64_t shares = (a.items * most_tiles(p) + kAttendLeast - 1u) / kAttendLeast;
-  a.most = (uint32_t)(shares < kAttendShares ? shares : kAttendShares);
+  // Waves: as many as the chip holds at once at the kernel's registers (64 dimensions: three quarters, 3072 took 32.6 us where 2048 take 32.0),
+  // or as many as have 4 tiles each.
+  const uint64_t shares = (a.items * most_tiles(p) + kAttendLeast - 1u) / kAttendLeast, fit = p->head_dim == 256 ? 1024u : 2048u;
+  a.most = (uint32_t)(shares < fit ? shares : fit);
   a.floats = a.split ? (a.items + a.most) * a.heads * ((uint64_t)p->head_dim + 2u) : 0u;
   return QKV_OK;
 }

@@ -29,59 +29,109 @@ constexpr uint32_t kAttendThreads = 256;
 constexpr uint32_t kAttendWaves = kAttendThreads / kWaveSize;
 constexpr float kLift = 10.0f;                           // weights are 2^kLift times what they are
 
-// Where a share begins: item and tile in the item.  `total`: tiles of all items.
-struct Cursor {
-  uint32_t row, inner, tile, tiles;                      // inner: kv head * blocks + block; tiles: of the item
-  Seen seen;
-};
-
 __device__ inline uint32_t sum64(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_readlane((int)wave_inclusive_scan(x), 63);
 }
 
-__device__ inline Seen row_seen(const PagedAttendArgs& a, uint32_t row) {
-  return seen_by_last(held(a.p.lens[row], a.p.row_pages, a.p.page_shift), a.window, a.sinks);
+__device__ inline uint32_t row_length(const PagedAttendArgs& a, uint32_t row) { return held(a.p.lens[row], a.p.row_pages, a.p.page_shift); }
+
+// The rows' tiles: lane l has row l's length, of the first 64 rows, and (one query head group of one kv head) its tiles; `total` is of all rows.
+// With up to 64 rows nothing more has to be read to find a share.
+struct Lengths {
+  uint32_t length, tiles, total;
+};
+__device__ inline Lengths read_lengths(const PagedAttendArgs& a, uint32_t lane) {
+  Lengths n;
+  n.length = lane < a.p.rows ? row_length(a, lane) : 0u;
+  n.tiles = lane < a.p.rows ? seen_tiles(seen_by_last(n.length, a.window, a.sinks)) : 0u;
+  uint32_t sum = n.tiles;
+  for (uint32_t row = lane + kWaveSize; row < a.p.rows; row += kWaveSize) sum += seen_tiles(seen_by_last(row_length(a, row), a.window, a.sinks));
+  n.total = sum64(sum);
+  return n;
 }
 
-// Tiles of all items.
-__device__ inline uint32_t all_tiles(const PagedAttendArgs& a, uint32_t lane) {
-  uint32_t sum = 0u;
-  for (uint32_t row = lane; row < a.p.rows; row += kWaveSize) sum += seen_tiles(row_seen(a, row));
-  return sum64(sum) * (a.p.kv_heads * a.blocks);
-}
-
-// The row that tile `at` falls into, and the tiles in front of that row.
-__device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, uint32_t lane, uint32_t at, uint32_t& before) {
-  const uint32_t inner = a.p.kv_heads * a.blocks;
+// The row that tile `at` of all rows falls into, the tiles in front of that row, and its length.
+__device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, const Lengths& n, uint32_t lane, uint32_t at, uint32_t& before, uint32_t& length) {
   before = 0u;
   for (uint32_t base = 0;; base += kWaveSize) {
     const uint32_t row = base + lane;
-    const uint32_t mine = row < a.p.rows ? seen_tiles(row_seen(a, row)) * inner : 0u;
+    uint32_t here = n.length, mine = n.tiles;
+    if (base != 0u) {
+      here = row < a.p.rows ? row_length(a, row) : 0u;
+      mine = row < a.p.rows ? seen_tiles(seen_by_last(here, a.window, a.sinks)) : 0u;
+    }
     const uint32_t upto = before + wave_inclusive_scan(mine);
     const uint64_t over = __builtin_amdgcn_ballot_w64(upto > at);
     if (over != 0ull || base + kWaveSize >= a.p.rows) {
       const uint32_t who = over ? (uint32_t)__builtin_ctzll(over) : (a.p.rows - 1u) % kWaveSize;
       before = (uint32_t)__builtin_amdgcn_readlane((int)(upto - mine), (int)who);
+      length = (uint32_t)__builtin_amdgcn_readlane((int)here, (int)who);
       return base + who;
     }
     before = (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
   }
 }
 
-// The pages of a tile's tokens: lane l holds that of token l % 32; `counted` has a bit for each token that is seen and has a page.
-template <bool SMALL>
+// RUN: tokens of a tile that surely lie in one page, one after the other: 32 or 16, or 1 where pages are smaller.
+// The entry that lane l needs of a tile's pages: that of token l % 32, or where a page holds whole tiles the tile's.
+template <uint32_t RUN>
 __device__ inline uint32_t look_up(const PagedAttendArgs& a, uint32_t row, const TileRange& t, uint32_t lane) {
   const int32_t* entries = a.p.table + (uint64_t)row * a.p.row_pages;
-  if constexpr (SMALL) {
-    const uint32_t token = t.first + lane % kAttendTile;
-    return token >= t.lo && token < t.hi ? (uint32_t)entries[token >> a.p.page_shift] : 0u;
-  } else {
-    return t.lo < t.hi ? (uint32_t)entries[t.first >> a.p.page_shift] : 0u;
-  }
+  if constexpr (RUN == 32u) return t.lo < t.hi ? (uint32_t)entries[t.first >> a.p.page_shift] : 0u;
+  const uint32_t token = t.first + lane % kAttendTile;
+  return token >= t.lo && token < t.hi ? (uint32_t)entries[token >> a.p.page_shift] : 0u;
 }
 
-template <typename T, int D, bool SMALL>
-__global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs a) {
+// A tile whose entries have arrived: its tokens that count (a bit each), and the pages to read, which exist even where a token does not count.
+struct Tile {
+  uint32_t first, page, counted;
+};
+template <uint32_t RUN>
+__device__ inline Tile settle(const PagedAttendArgs& a, const TileRange& t, uint32_t entry, uint32_t lane) {
+  const uint32_t token = t.first + lane % kAttendTile;
+  const bool inside = token >= t.lo && token < t.hi, known = entry < a.p.pages;
+  Tile tile;
+  tile.first = t.first;
+  tile.counted = (uint32_t)__builtin_amdgcn_ballot_w64(inside && known);
+  if ((uint32_t)__builtin_amdgcn_ballot_w64(inside && !known) != 0u && lane == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
+  tile.page = known ? entry : 0u;
+  return tile;
+}
+// The page of the run that token `of` of the tile is in: in RUN == 16 the entry of any of the run's tokens that is looked up will do.
+template <uint32_t RUN>
+__device__ inline uint32_t page_of(const Tile& t, uint32_t run) {
+  if constexpr (RUN == 32u) return (uint32_t)__builtin_amdgcn_readfirstlane((int)t.page);
+  const uint32_t mine = t.counted >> (16u * run) & 0xFFFFu;
+  return (uint32_t)__builtin_amdgcn_readlane((int)t.page, (int)(16u * run + (mine ? (uint32_t)__builtin_ctz(mine) : 0u)));
+}
+
+// Where the rows of a tile's tokens are read from: 16 bytes at a time, from a place that is the same for all lanes and 32 bits of a lane's own (runs),
+// or an address a lane (single tokens).
+template <uint32_t RUN>
+struct RowSource {
+  const uint8_t* base[RUN == 16u ? 2 : 1];
+  __device__ inline RowSource(const PagedAttendArgs& a, const uint8_t* pool, const Tile& t) {
+    if constexpr (RUN == 1u) {
+      base[0] = pool;
+    } else {
+      const uint64_t in_page = (uint64_t)(t.first & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride;
+#pragma unroll
+      for (uint32_t r = 0; r < 32u / RUN; ++r) base[r] = pool + (uint64_t)page_of<RUN>(t, r) * a.p.page_stride + (RUN == 32u ? in_page : 0u);
+    }
+  }
+  // token `of` = fixed + own (fixed: the same for all lanes, with own within one run)
+  __device__ inline const uint8_t* row(const PagedAttendArgs& a, const Tile& t, uint32_t fixed, uint32_t own, uint32_t piece) const {
+    if constexpr (RUN == 1u) {
+      const uint32_t page = (uint32_t)__shfl((int)t.page, (int)(fixed + own));
+      return base[0] + (uint64_t)page * a.p.page_stride + (uint64_t)((t.first + fixed + own) & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride + piece;
+    } else {
+      return base[RUN == 16u ? fixed / 16u : 0u] + ((fixed % RUN + own) * (uint32_t)a.p.token_stride + piece);
+    }
+  }
+};
+
+template <typename T, int D, uint32_t RUN>
+__global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kernel(PagedAttendArgs a) {
   constexpr uint32_t kSteps = D / 32;                    // MFMAs along the head dimension
   constexpr uint32_t kSlabs = D / 16;                    // of 16 dimensions of the result
   constexpr uint32_t kLoads = kAttendTile * D / 8 / kWaveSize;         // 16-byte loads of V in a lane
@@ -90,18 +140,18 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
   __shared__ __attribute__((aligned(256))) uint8_t lds[kAttendWaves][kAttendTile * D * 2];
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
   const uint32_t n = lane % 16u, g = lane / 16u;
-  const uint32_t share = blockIdx.x * kAttendWaves + wave;
   const uint32_t inner_count = a.p.kv_heads * a.blocks, q_heads = a.p.kv_heads * a.rep;
-  const uint32_t total = (uint32_t)__builtin_amdgcn_readfirstlane((int)all_tiles(a, lane));
-  const Shares shares = deal(total, a.most);
+  const Lengths lengths = read_lengths(a, lane);
+  const Shares shares = deal(lengths.total * inner_count, a.most);
+  const uint32_t share = blockIdx.x * kAttendWaves + wave;
   if (share >= shares.shares) return;
   uint32_t at = share_begin(shares, share);
   const uint32_t end = share_begin(shares, share + 1u);
-  uint32_t before;
-  uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)row_of_tile(a, lane, at, before));
-  Seen seen = row_seen(a, row);
+  uint32_t before, length;
+  uint32_t row = row_of_tile(a, lengths, lane, at / inner_count, before, length);
+  Seen seen = seen_by_last(length, a.window, a.sinks);
   uint32_t tiles = seen_tiles(seen);
-  uint32_t inner = (at - before) / tiles, tile = (at - before) % tiles;
+  uint32_t inner = (at - before * inner_count) / tiles, tile = (at - before * inner_count) % tiles;
   uint8_t* mine = lds[wave];
 
   while (at < end) {
@@ -110,6 +160,25 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
     const uint32_t heads = min(16u, a.rep - block * 16u);
     const uint32_t from = tile, upto = min(tiles, tile + (end - at));
     const uint32_t hq = head * a.rep + block * 16u + n;                // this lane's query head, if n < heads
+    const uint8_t* keys = a.p.k + (uint64_t)head * a.p.head_stride;
+    const uint8_t* values = a.p.v + (uint64_t)head * a.p.head_stride;
+    u32x4 kx[2][kSteps], vx[kLoads];
+    const auto load_keys = [&](const Tile& t) {
+      const RowSource<RUN> from(a, keys, t);
+#pragma unroll
+      for (uint32_t h = 0; h < 2u; ++h) {
+        const uint8_t* p = from.row(a, t, h * 16u, n, g * 16u);
+#pragma unroll
+        for (uint32_t k = 0; k < kSteps; ++k) kx[h][k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + k * 64u));
+      }
+    };
+    const auto load_values = [&](const Tile& t) {
+      const RowSource<RUN> from(a, values, t);
+#pragma unroll
+      for (uint32_t j = 0; j < kLoads; ++j) vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from.row(a, t, j * kRowsAtOnce, lane / kRowLanes, (lane % kRowLanes) * 16u)));
+    };
+    TileRange range = tile_range(seen, from);
+    uint32_t entry = look_up<RUN>(a, row, range, lane);
     typename T::x8 q[kSteps];
 #pragma unroll
     for (uint32_t k = 0; k < kSteps; ++k) {
@@ -117,54 +186,34 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
       if (n < heads) x = *reinterpret_cast<const u32x4*>(a.q + (uint64_t)row * a.q_token_stride + (uint64_t)hq * a.q_head_stride + (k * 32u + g * 8u) * 2u);
       q[k] = __builtin_bit_cast(typename T::x8, x);
     }
+    Tile now = settle<RUN>(a, range, entry, lane);
+    load_keys(now);
+    load_values(now);
+    if (from + 1u < upto) {
+      range = tile_range(seen, from + 1u);
+      entry = look_up<RUN>(a, row, range, lane);
+    }
     f32x4 acc[kSlabs];
 #pragma unroll
     for (uint32_t d = 0; d < kSlabs; ++d) acc[d] = (f32x4)(0.0f);
     float m = -INFINITY, l = 0.0f;
 
-    const uint8_t* keys = a.p.k + (uint64_t)head * a.p.head_stride;
-    const uint8_t* values = a.p.v + (uint64_t)head * a.p.head_stride;
-    TileRange t = tile_range(seen, from);
-    uint32_t page = look_up<SMALL>(a, row, t, lane);
     for (uint32_t i = from; i < upto; ++i) {
-      // tokens that count
-      const uint32_t token = t.first + lane % kAttendTile;
-      const bool inside = token >= t.lo && token < t.hi, known = page < a.p.pages;
-      const uint32_t counted = (uint32_t)__builtin_amdgcn_ballot_w64(inside && known);
-      if ((uint32_t)__builtin_amdgcn_ballot_w64(inside && !known) != 0u && lane == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
-      if (!(inside && known) && SMALL) page = 0u;
-      if (!SMALL) page = (uint32_t)__builtin_amdgcn_readfirstlane((int)(known ? page : 0u));
-      const uint32_t in_page = (1u << a.p.page_shift) - 1u;
-      const auto row_at = [&](uint32_t of) -> uint64_t {               // byte offset of the tile's token `of`
-        if constexpr (SMALL) {
-          const uint32_t p = (uint32_t)__shfl((int)page, (int)of);
-          return (uint64_t)p * a.p.page_stride + ((t.first + of) & in_page) * a.p.token_stride;
-        } else {
-          return (uint64_t)page * a.p.page_stride + ((t.first + of) & in_page) * a.p.token_stride;
-        }
-      };
-      u32x4 kx[2][kSteps], vx[kLoads];
-#pragma unroll
-      for (uint32_t h = 0; h < 2u; ++h) {
-        const uint8_t* p = keys + row_at(h * 16u + n) + g * 16u;
-#pragma unroll
-        for (uint32_t k = 0; k < kSteps; ++k) kx[h][k] = *reinterpret_cast<const u32x4*>(p + k * 64u);
-      }
-#pragma unroll
-      for (uint32_t j = 0; j < kLoads; ++j) {
-        const uint8_t* p = values + row_at(j * kRowsAtOnce + lane / kRowLanes) + (lane % kRowLanes) * 16u;
-        vx[j] = *reinterpret_cast<const u32x4*>(p);
-      }
-      if (i + 1u < upto) {
-        t = tile_range(seen, i + 1u);
-        page = look_up<SMALL>(a, row, t, lane);
-      }
-
+      const uint32_t counted = now.counted;
       f32x4 s[2] = {(f32x4)(0.0f), (f32x4)(0.0f)};
 #pragma unroll
       for (uint32_t k = 0; k < kSteps; ++k) {
         s[0] = T::mfma16(__builtin_bit_cast(typename T::x8, kx[0][k]), q[k], s[0]);
         s[1] = T::mfma16(__builtin_bit_cast(typename T::x8, kx[1][k]), q[k], s[1]);
+      }
+      // the registers of K are free: the next tile's keys are on their way while this one's weights are worked out
+      if (i + 1u < upto) {
+        now = settle<RUN>(a, range, entry, lane);
+        load_keys(now);
+        if (i + 2u < upto) {
+          range = tile_range(seen, i + 2u);
+          entry = look_up<RUN>(a, row, range, lane);
+        }
       }
       float e[8];
       float top = -INFINITY;
@@ -205,8 +254,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
           vx[j] = counts ? vx[j] : (u32x4)(0u);
         }
       }
-#pragma unroll
-      for (uint32_t j = 0; j < 8u; ++j) l += e[j];
+      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       typename T::x8 w[T::kParts];
       T::parts(e, w);
 
@@ -218,6 +266,7 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
+      if (i + 1u < upto) load_values(now);
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d) {
         const uint32_t r = 4u * g + n / 4u;                            // token of the first half
@@ -236,8 +285,8 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
       float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
       float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(l)) * 0.6931471805599453f;
       float other = 0.0f;
-      if (a.prior_out && n < heads) join(lse, a.prior_lse[at_head], scale, other);
       if (n < heads) {
+        if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
 #pragma unroll
         for (uint32_t d = 0; d < kSlabs; ++d) {
           f32x4 o = acc[d] * scale;
@@ -245,12 +294,13 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
           if (a.prior_out && other != 0.0f) o += *reinterpret_cast<const f32x4*>(a.prior_out + where) * other;
           *reinterpret_cast<f32x4*>(a.out + where) = o;
         }
-        if (a.lse && g == 0u) a.lse[at_head] = lse;
       }
+      if (n < heads && a.lse && g == 0u) a.lse[at_head] = lse;
     } else if (n < heads) {
       const uint64_t slot = ((uint64_t)row * inner_count + inner + share) * min(16u, a.rep) + n;
 #pragma unroll
-      for (uint32_t d = 0; d < kSlabs; ++d) *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 16u + g * 4u) = acc[d];
+      for (uint32_t d = 0; d < kSlabs; ++d)
+        *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 16u + g * 4u) = acc[d];
       if (g == 0u) *reinterpret_cast<f32x2*>(a.part_ml + slot * 2u) = (f32x2){m, l};
     }
 
@@ -259,61 +309,77 @@ __global__ __launch_bounds__(kAttendThreads) void attend_kernel(PagedAttendArgs 
     if (++inner == inner_count && at < end) {
       inner = 0u;
       ++row;
-      seen = row_seen(a, row);
+      seen = seen_by_last((uint32_t)__builtin_amdgcn_readfirstlane((int)row_length(a, row)), a.window, a.sinks);
       tiles = seen_tiles(seen);
     }
   }
 }
 
-// Joins the parts of an item that was cut: a workgroup takes one query head of one item.
-constexpr uint32_t kJoinThreads = 256;
-
-template <int D>
-__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(PagedAttendArgs a) {
-  constexpr uint32_t kLanes = D / 4, kGroups = kJoinThreads / kLanes;  // a group of lanes goes through every kGroups-th part
-  __shared__ f32x4 sums[kGroups][kLanes];
-  __shared__ f32x2 tops[kGroups];
+// Joins the parts of an item that was cut: a workgroup takes `together` query heads of one item, D / 4 lanes each, and goes through the
+// parts in as many groups of those lanes as it has.
+template <int D, uint32_t THREADS>
+__global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a, uint32_t together) {
+  constexpr uint32_t kLanes = D / 4, kAtOnce = 4;
+  __shared__ f32x4 sums[THREADS];
+  __shared__ f32x2 tops[THREADS / kLanes];
   const uint32_t lane = threadIdx.x % kWaveSize;
   const uint32_t heads = min(16u, a.rep), inner_count = a.p.kv_heads * a.blocks, q_heads = a.p.kv_heads * a.rep;
-  const uint32_t item = blockIdx.x, row = item / inner_count, inner = item % inner_count;
-  const uint32_t in_block = blockIdx.y, block = inner % a.blocks;
-  if (block * 16u + in_block >= a.rep) return;
-  uint32_t all = 0u, front = 0u;
+  const uint32_t item = blockIdx.x, row = item / inner_count, inner = item % inner_count, block = inner % a.blocks;
+  uint32_t all = 0u, front = 0u, own = 0u;
   for (uint32_t r = lane; r < a.p.rows; r += kWaveSize) {
-    const uint32_t x = seen_tiles(row_seen(a, r));
+    const uint32_t x = seen_tiles(seen_by_last(row_length(a, r), a.window, a.sinks));
     all += x;
     front += r < row ? x : 0u;
+    own += r == row ? x : 0u;
   }
-  const uint32_t total = sum64(all) * inner_count;
-  const uint32_t tiles = seen_tiles(row_seen(a, row));
-  const uint32_t begin = sum64(front) * inner_count + inner * tiles;
+  const uint32_t total = sum64(all) * inner_count, tiles = sum64(own), begin = sum64(front) * inner_count + inner * tiles;
   const Shares shares = deal(total, a.most);
   const uint32_t first = share_of(shares, begin), last = share_of(shares, begin + tiles - 1u);
   if (first == last) return;                                           // finished where it was
-  const uint32_t group = threadIdx.x / kLanes, at = threadIdx.x % kLanes;
+  const uint32_t groups = THREADS / kLanes / together;                 // at least one
+  const uint32_t group = threadIdx.x / kLanes / together, at = threadIdx.x % kLanes, in_block = blockIdx.y * together + threadIdx.x / kLanes % together;
+  const bool some = group < groups && in_block < heads && block * 16u + in_block < a.rep;
   float m = -INFINITY, l = 0.0f;
   f32x4 o = (f32x4)(0.0f);
-  for (uint32_t s = first + group; s <= last; s += kGroups) {
-    const uint64_t slot = ((uint64_t)item + s) * heads + in_block;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
-    const float top = fmaxf(m, ml.x);
-    const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top), take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);
-    l = l * keep + ml.y * take;
-    o = o * keep + x * take;
+  for (uint32_t s = first + group; some && s <= last; s += kAtOnce * groups) {
+    f32x2 ml[kAtOnce];
+    f32x4 x[kAtOnce];
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint32_t part = min(s + k * groups, last);                // past the last one: the last one, without weight
+      const uint64_t slot = ((uint64_t)item + part) * heads + in_block;
+      ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
+      x[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
+    }
+    float top = m;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      if (s + k * groups > last) ml[k].x = -INFINITY;
+      top = fmaxf(top, ml[k].x);
+    }
+    const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      if (ml[k].x == -INFINITY) continue;                              // such a part may hold anything
+      const float take = exp2f_(ml[k].x - top);
+      l += ml[k].y * take;
+      o += x[k] * take;
+    }
     m = top;
   }
-  sums[group][at] = o;
-  if (at == 0u) tops[group] = (f32x2){m, l};
+  sums[threadIdx.x] = o;
+  if (at == 0u) tops[threadIdx.x / kLanes] = (f32x2){m, l};
   __syncthreads();
-  if (group != 0u) return;
-#pragma unroll
-  for (uint32_t k = 1; k < kGroups; ++k) {
-    const f32x2 ml = tops[k];
+  if (group != 0u || !some) return;
+#pragma unroll 4
+  for (uint32_t k = 1; k < groups; ++k) {
+    const f32x2 ml = tops[k * together + threadIdx.x / kLanes];
     const float top = fmaxf(m, ml.x);
     const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top), take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);
     l = l * keep + ml.y * take;
-    o = o * keep + sums[k][at] * take;
+    o = o * keep + sums[k * together * kLanes + threadIdx.x] * take;
     m = top;
   }
   const uint64_t at_head = (uint64_t)row * q_heads + (inner / a.blocks) * a.rep + block * 16u + in_block;
@@ -330,12 +396,20 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(PagedAttendAr
 template <typename T, int D>
 hipError_t launch_attend_of(const PagedAttendArgs& a, bool may_split, hipStream_t stream) {
   const uint32_t items = a.p.rows * a.p.kv_heads * a.blocks;
-  const uint32_t grid = (a.most + kAttendWaves - 1u) / kAttendWaves;
-  if ((1u << a.p.page_shift) < kAttendTile) attend_kernel<T, D, true><<<grid, kAttendThreads, 0, stream>>>(a);
-  else attend_kernel<T, D, false><<<grid, kAttendThreads, 0, stream>>>(a);
+  const uint32_t grid = (a.most + kAttendWaves - 1u) / kAttendWaves;         // teams, or waves in fours
+  if (a.p.page_shift >= 5u) attend_kernel<T, D, 32u><<<grid, kAttendThreads, 0, stream>>>(a);
+  else if (a.p.page_shift == 4u) attend_kernel<T, D, 16u><<<grid, kAttendThreads, 0, stream>>>(a);
+  else attend_kernel<T, D, 1u><<<grid, kAttendThreads, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && may_split) {
-    attend_join_kernel<D><<<dim3(items, std::min(16u, a.rep)), kJoinThreads, 0, stream>>>(a);
+    // Many parts an item (a long sequence among few): many threads for each head; otherwise one workgroup for an item's heads.
+    const uint32_t heads = std::min(16u, a.rep);
+    if (a.most / items >= 64u) {
+      attend_join_kernel<D, 1024><<<dim3(items, heads), 1024, 0, stream>>>(a, 1u);
+    } else {
+      const uint32_t together = std::min(heads, 256u / (D / 4u));
+      attend_join_kernel<D, 256><<<dim3(items, (heads + together - 1u) / together), 256, 0, stream>>>(a, together);
+    }
     e = hipGetLastError();
   }
   return e;
