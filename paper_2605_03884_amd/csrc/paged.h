@@ -140,7 +140,7 @@ struct PagedPromptArgs {
   const uint8_t* q;
   uint64_t q_token_stride, q_head_stride;                // bytes
   const int32_t* starts;
-  uint32_t tokens, rep, per;                             // per: query tokens of a tile
+  uint32_t tokens, rep, per, waves;                      // per: query tokens of a tile, waves: of a workgroup, 32 (token, head) pairs each
   uint32_t window, sinks;
   float scale_log2;                                      // the softmax scale's absolute value times log2(e), above 0
   uint32_t flip;                                         // the scale is negative: q's signs are turned instead

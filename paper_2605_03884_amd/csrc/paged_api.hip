@@ -7,7 +7,6 @@ using namespace qkv;
 
 namespace {
 
-constexpr uint32_t kPromptRows = 128;         // (query token, query head) pairs of a prompt tile
 constexpr uint32_t kPromptTarget = 512;       // workgroups the prompt kernel's work is split into, where there are fewer query tiles
 
 bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
@@ -121,13 +120,15 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
 }
 
 struct PromptPlan {
-  uint32_t rep, per, splits;
+  uint32_t rep, per, waves, splits;
   uint64_t floats;
 };
 int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
   if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
   a.rep = (uint32_t)(q_heads / p->kv_heads);
-  a.per = kPromptRows / a.rep;
+  // Tiles of 256 pairs (8 waves) where there are enough of them for all CUs, of 128 otherwise.
+  a.waves = p->head_dim <= 128 && (uint64_t)tokens * (uint64_t)q_heads >= 256u * 256u ? 8u : 4u;
+  a.per = a.waves * 32u / a.rep;
   const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
   if (tiles >= (1ull << 31)) return QKV_ERR_SHAPE;
   // Few query tiles: the keys are split until there are about two workgroups a CU, into shares of at least 256 tokens.
@@ -303,6 +304,7 @@ int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   a.tokens = (uint32_t)query->tokens;
   a.rep = plan.rep;
   a.per = plan.per;
+  a.waves = plan.waves;
   a.window = window_of(pages, query->window);
   a.sinks = a.window ? (uint32_t)query->sinks : 0u;
   a.scale_log2 = (float)(std::fabs((double)query->softmax_scale) * 1.4426950408889634);
