@@ -18,7 +18,6 @@ namespace qkv {
 
 constexpr uint32_t kAttendTile = 32;         // tokens a wave of the decode kernel takes at a time
 constexpr uint32_t kAttendLeast = 4;         // tiles a share has at least, where the work is split at all
-constexpr uint32_t kPromptKeys = 64;         // tokens of keys a workgroup of the prompt kernel takes at a time
 constexpr uint32_t kMaxRows = 65536;         // sequences of a table
 
 // The tokens a query at the last position of `length` sees: [0, sink_end) and [begin, length).
@@ -140,7 +139,7 @@ struct PagedPromptArgs {
   const uint8_t* q;
   uint64_t q_token_stride, q_head_stride;                // bytes
   const int32_t* starts;
-  uint32_t tokens, rep, per, waves;                      // per: query tokens of a tile, waves: of a workgroup, 32 (token, head) pairs each
+  uint32_t tokens, rep, per, waves;                      // per: query tokens of a tile; waves: of a workgroup, 32 (token, head) pairs each
   uint32_t window, sinks;
   float scale_log2;                                      // the softmax scale's absolute value times log2(e), above 0
   uint32_t flip;                                         // the scale is negative: q's signs are turned instead

@@ -7,7 +7,6 @@ using namespace qkv;
 
 namespace {
 
-constexpr uint32_t kPromptTarget = 512;       // workgroups the prompt kernel's work is split into, where there are fewer query tiles
 
 bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
@@ -126,14 +125,15 @@ struct PromptPlan {
 int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
   if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
   a.rep = (uint32_t)(q_heads / p->kv_heads);
-  // Tiles of 256 pairs (8 waves) where there are enough of them for all CUs, of 128 otherwise.
-  a.waves = p->head_dim <= 128 && (uint64_t)tokens * (uint64_t)q_heads >= 256u * 256u ? 8u : 4u;
-  a.per = a.waves * 32u / a.rep;
+  // Tiles of 256 pairs, where the mean sequence has more than 128 of them to a kv head; 256 dimensions have no registers for more than 128.
+  a.waves = p->head_dim <= 128 && tokens * a.rep > 128 * (int64_t)p->rows ? 8u : 4u;
+  a.per = 32u * a.waves / a.rep;
   const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
   if (tiles >= (1ull << 31)) return QKV_ERR_SHAPE;
-  // Few query tiles: the keys are split until there are about two workgroups a CU, into shares of at least 256 tokens.
-  const uint64_t room = ((uint64_t)p->row_pages * (uint64_t)p->page_tokens + 255u) / 256u;
-  uint64_t n = kPromptTarget / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
+  // Few query tiles: the keys are split until there is a workgroup of 8 waves or two of 4 to a CU, into shares of at least 512 tokens.  (61 tokens of 32
+  // heads behind 32768: 75 us with 128 workgroups, 67 with 256, 87 with 384.)
+  const uint64_t room = (uint64_t)p->row_pages * (uint64_t)p->page_tokens / 512u;
+  uint64_t n = (a.waves == 8u ? 256u : 512u) / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
   if (n > room) n = room;
   if (n > 64u) n = 64u;
   a.splits = n < 2u ? 1u : (uint32_t)n;

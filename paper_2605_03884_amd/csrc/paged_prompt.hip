@@ -7,7 +7,7 @@
 //
 // A tile of 64 keys, one wave (lane = 32 h + n; n is the lane's pair):
 //   staging  rows of K and V go from memory into registers and on into LDS, K two tiles ahead of its use and V one, each into one of two
-//            places: K in 16-byte pieces exchanged by token, V in 64-byte pieces, so that no read below meets a bank twice.
+//            places.
 //   scores   S^T = K Q^T on v_mfma_f32_32x32x16: a lane gets 32 scores of its own pair.
 //   softmax  in the lane, and with the lane 32 further on.  m follows the true maximum only when that has grown by 2^8: sums are
 //            kept relative to m, and the weights have 2^7 of room below and 2^8 above before fp16 could overflow.
@@ -24,21 +24,16 @@ namespace {
 
 constexpr float kLift = 7.0f, kSlack = 8.0f;
 
-// Waves a SIMD holds at once: what its 512 registers allow.
-constexpr uint32_t prompt_waves_a_simd(int D, uint32_t waves) { return D == 256 ? 1u : waves == 8u ? 2u : D == 64 ? 2u : 1u; }
+// Rows of K and V in LDS are longer than they need to be, by 16 and 64 bytes: 16 lanes that read a piece of 16 bytes of as many rows of K, and 32 that
+// read 64 bytes of four rows of V through the transposing read, then meet every bank once.
 
-// Where the 16-byte piece `chunk` of token `token`'s row of K stands in LDS.
-template <int D>
-__device__ inline uint32_t key_at(uint32_t token, uint32_t chunk) {
-  const uint32_t turn = D == 64 ? (token >> 1) & 7u : token & 15u;
-  return token * (D * 2u) + (chunk ^ turn) * 16u;
-}
-// The same for V, by its piece of 64 bytes.
-template <int D>
-__device__ inline uint32_t value_at(uint32_t token, uint32_t piece) {
-  const uint32_t turn = D == 64 ? (token >> 1) & 1u : token & 3u;
-  return token * (D * 2u) + (piece ^ turn) * 64u;
-}
+// Keys of a tile: as many as leave LDS for two workgroups of 4 waves a CU, or one of 8.
+constexpr uint32_t prompt_keys(uint32_t waves) { return waves == 8u ? 64u : 32u; }
+// Waves a SIMD holds at once: what its 512 registers allow.
+constexpr uint32_t prompt_waves_a_simd(int D) { return D == 256 ? 1u : 2u; }
+
+constexpr uint32_t key_row(int D) { return D * 2u + 16u; }
+constexpr uint32_t value_row(int D) { return D * 2u + 64u; }
 
 // Takes what is infinite or no number out of eight values; whether there was any.
 template <typename T>
@@ -57,13 +52,15 @@ __device__ inline bool take_out(u32x4& x) {
 }
 
 template <typename T, int D, uint32_t RUN, bool SPLIT, uint32_t WAVES>
-__global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D, WAVES)) void prompt_kernel(PagedPromptArgs a) {
+__global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void prompt_kernel(PagedPromptArgs a) {
   constexpr uint32_t kThreads = WAVES * kWaveSize;
-  constexpr uint32_t kKeys = kPromptKeys, kChunks = D / 8;             // 16-byte pieces of a row
+  constexpr uint32_t kKeys = prompt_keys(WAVES), kHalves = kKeys / 32u;    // keys of a tile; scores are worked out 32 keys at a time
+  constexpr uint32_t kPlaces = kHalves + 1u;                           // tiles of K in LDS
+  constexpr uint32_t kChunks = D / 8;                                  // 16-byte pieces of a row
   constexpr uint32_t kLoads = kKeys * kChunks / kThreads;              // of them a thread loads, of K and of V
   constexpr uint32_t kRowsAtOnce = kThreads / kChunks;
   constexpr uint32_t kSteps = D / 16, kSlabs = D / 32;
-  __shared__ __attribute__((aligned(256))) uint8_t k_place[2][kKeys * D * 2], v_place[2][kKeys * D * 2];
+  __shared__ __attribute__((aligned(256))) uint8_t k_place[kPlaces][kKeys * key_row(D)], v_place[2][kKeys * value_row(D)];
   __shared__ uint32_t taken_out;                                       // somebody took something out of the values
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
   const uint32_t n = lane % 32u, h = lane / 32u;
@@ -94,16 +91,25 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D, WAVES)) v
   const uint32_t first_tile = SPLIT ? (uint32_t)((uint64_t)tiles * blockIdx.y / a.splits) : 0u;
   const uint32_t last_tile = SPLIT ? (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / a.splits) : tiles;
   const auto tile_at = [&](uint32_t i) -> int32_t { return (int32_t)((i < head ? i : body + (i - head)) * kKeys); };
-  // whether every one of the queries at places [lo, hi] sees all of the tile's keys
-  const auto whole = [&](int32_t t, int32_t lo, int32_t hi) { return t + (int32_t)kKeys - 1 <= lo && (window == 0 || t > hi - window || t + (int32_t)kKeys <= sinks); };
+  // Tiles [from, from + count) are seen whole by all queries at places [lo, hi]; those of the sinks are not counted among them.
+  struct Range {
+    uint32_t from, count;
+  };
+  const auto whole = [&](int32_t lo, int32_t hi) -> Range {
+    const int32_t shift = (int32_t)head - (int32_t)body, win = hi - window + 1;
+    const int32_t from = window != 0 && win > 0 ? max(shift + (win + (int32_t)kKeys - 1) / (int32_t)kKeys, (int32_t)head) : (int32_t)head;
+    const int32_t upto = lo >= 0 ? shift + (lo + 1) / (int32_t)kKeys : 0;
+    return Range{(uint32_t)from, upto > from ? (uint32_t)(upto - from) : 0u};
+  };
+  const auto holds = [](const Range& r, uint32_t i) { return i - r.from < r.count; };
+
   // the lane's pair
-  const uint32_t pair = wave * 32u + n, token = pair / a.rep, head_in = pair % a.rep;
+  const uint32_t pair = wave * 32u + n, token = pair / a.rep, hq = kv_head * a.rep + pair % a.rep;
   const bool live = token < here;
   const int32_t mine = live ? base + (int32_t)token : -1;
   const uint32_t wave_first = wave * 32u / a.rep, wave_last = min((wave * 32u + 31u) / a.rep, here - 1u);
-  const int32_t wave_lo = base + (int32_t)wave_first, wave_hi = base + (int32_t)wave_last;
+  const Range whole_to_all = whole(base, reach - 1), whole_to_wave = whole(base + (int32_t)wave_first, base + (int32_t)wave_last);
   const uint64_t query = (uint64_t)(uint32_t)start + skip + token;
-  const uint32_t hq = kv_head * a.rep + head_in;
   typename T::x8 q[kSteps];
 #pragma unroll
   for (uint32_t k = 0; k < kSteps; ++k) {
@@ -115,7 +121,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D, WAVES)) v
   f32x16 acc[kSlabs];
 #pragma unroll
   for (uint32_t d = 0; d < kSlabs; ++d) acc[d] = (f32x16)(0.0f);
-  float m = -INFINITY, l = 0.0f;
+  float m = -INFINITY, l = 0.0f, less = 0.0f;                          // less: what is taken off in the exponent
 
   const uint8_t* keys = a.p.k + (uint64_t)kv_head * a.p.head_stride;
   const uint8_t* values = a.p.v + (uint64_t)kv_head * a.p.head_stride;
@@ -123,235 +129,298 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D, WAVES)) v
   const uint32_t in_page = (1u << a.p.page_shift) - 1u, my_row = threadIdx.x / kChunks, my_chunk = threadIdx.x % kChunks;
   u32x4 kx[kLoads], vx[kLoads];
 
-  // A tile goes through four hands: its entries are looked up, its rows are loaded, stored to LDS, worked on; each a tile ahead of the next.
-  // Lane l has token t + l's entry.  Nobody sees the tokens of `hidden` (they may be anything); those of `lost` have no page.
+  // A tile goes through four hands: its entries are looked up, its rows are loaded, stored to LDS, worked on.  Lane l has token t + l's entry.
   const auto seen_by_some = [&](int32_t key) { return key < reach && (key >= win_lo || key < (int32_t)sink_end); };
   const auto look_up = [&](uint32_t i) -> uint32_t {
-    const int32_t key = tile_at(i) + (int32_t)lane;
-    return seen_by_some(key) ? (uint32_t)entries[(uint32_t)key >> a.p.page_shift] : 0u;
+    const uint32_t key = min((uint32_t)(tile_at(i) + (int32_t)(lane % kKeys)), (uint32_t)reach - 1u);
+    return (uint32_t)entries[key >> a.p.page_shift];
   };
-  struct Source {
-    uint32_t page;                                                     // of token t + lane
-    uint64_t hidden, lost;
+  // Where the thread's rows of a tile are, in head 0: with pages of at least RUN tokens a place for each load that is the same for the wave, to which `own` is
+  // added, otherwise the thread's own.  Rows that nobody sees, and those without a page (`lost`, a bit a token), are read from page 0.
+  constexpr uint32_t kSpots = RUN == 64u ? 1u : kLoads;
+  struct Spots {
+    uint64_t at[kSpots];
   };
-  const auto settle = [&](uint32_t i, uint32_t entry) -> Source {
-    const bool wanted = seen_by_some(tile_at(i) + (int32_t)lane), known = entry < a.p.pages;
-    return Source{wanted && known ? entry : 0u, ~__builtin_amdgcn_ballot_w64(wanted && known), __builtin_amdgcn_ballot_w64(wanted && !known)};
-  };
-  const auto load = [&](const uint8_t* pool, uint32_t i, const Source& from, u32x4 (&x)[kLoads]) {
+  const uint32_t own = my_row % RUN * (RUN == 1u ? 0u : (uint32_t)a.p.token_stride) + my_chunk * 16u;
+  uint64_t lost = 0ull;
+  bool any_lost = false;
+  const auto settle = [&](uint32_t i, uint32_t entry) -> Spots {
     const int32_t t = tile_at(i);
-    if constexpr (RUN == 1u) {
+    uint32_t page = entry;
+    uint64_t there = ~0ull;
+    if (!(holds(whole_to_all, i) && __builtin_amdgcn_ballot_w64(entry >= a.p.pages) == 0ull)) {
+      const bool wanted = lane < kKeys && seen_by_some(t + (int32_t)lane), known = entry < a.p.pages;
+      there = __builtin_amdgcn_ballot_w64(wanted && known);
+      lost = __builtin_amdgcn_ballot_w64(wanted && !known);
+      any_lost = any_lost || lost != 0ull;
+      page = wanted && known ? entry : 0u;
+    }
+    Spots to;
+#pragma unroll
+    for (uint32_t j = 0; j < kSpots; ++j) {
+      const uint32_t of = j * kRowsAtOnce + my_row;                    // the row
+      if constexpr (RUN == 1u) {
+        to.at[j] = (uint64_t)(uint32_t)__shfl((int)page, (int)of) * a.p.page_stride + (uint64_t)(((uint32_t)t + of) & in_page) * a.p.token_stride;
+      } else {
+        // any token of the run that is there names the page; rows of a run lie one after the other
+        const uint32_t first = RUN == 64u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)(of / RUN * RUN));
+        const uint64_t here = there >> first & (RUN == 64u ? ~0ull : (1ull << (RUN % 64u)) - 1ull);
+        const uint32_t number = (uint32_t)__builtin_amdgcn_readlane((int)page, (int)(first + (here ? (uint32_t)__builtin_ctzll(here) : 0u)));
+        to.at[j] = (uint64_t)number * a.p.page_stride + (((uint32_t)t + first) & in_page) * (uint32_t)a.p.token_stride +
+                   (RUN == 16u && kRowsAtOnce < RUN ? j * kRowsAtOnce % RUN * (uint32_t)a.p.token_stride : 0u);
+      }
+    }
+    return to;
+  };
+  const auto load = [&](const uint8_t* pool, const Spots& from, u32x4 (&x)[kLoads]) {
+#pragma unroll
+    for (uint32_t j = 0; j < kLoads; ++j)
+      x[j] = *reinterpret_cast<const u32x4*>(pool + from.at[RUN == 64u ? 0u : j] + (own + (RUN == 64u ? j * kRowsAtOnce * (uint32_t)a.p.token_stride : 0u)));
+  };
+  uint8_t* const k_rows = k_place[0] + my_row * key_row(D) + my_chunk * 16u;
+  uint8_t* const v_rows = v_place[0] + my_row * value_row(D) + my_chunk * 16u;
+  const auto store_keys = [&](uint32_t at, const u32x4 (&x)[kLoads]) {
+#pragma unroll
+    for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(k_rows + at + j * kRowsAtOnce * key_row(D)) = x[j];
+  };
+  const auto store_values = [&](uint32_t i, uint32_t at) {
+    if (!holds(whole_to_all, i) || any_lost) {                         // only there can a value meet a weight that has to be nothing
+      if (any_lost) {
+        lost = 0ull;
+        settle(i, look_up(i));
+      }
 #pragma unroll
       for (uint32_t j = 0; j < kLoads; ++j) {
         const uint32_t of = j * kRowsAtOnce + my_row;
-        x[j] = *reinterpret_cast<const u32x4*>(pool + (uint64_t)(uint32_t)__shfl((int)from.page, (int)of) * a.p.page_stride +
-                                               (uint64_t)(((uint32_t)t + of) & in_page) * a.p.token_stride + my_chunk * 16u);
-      }
-    } else {
-      // rows of one run lie one after the other: a place that is the same for the wave and 32 bits of the lane's own
-      const uint32_t own = my_row % RUN * (uint32_t)a.p.token_stride + my_chunk * 16u;
-#pragma unroll
-      for (uint32_t j = 0; j < kLoads; ++j) {
-        const uint32_t run = RUN == 64u ? 0u : (uint32_t)__builtin_amdgcn_readfirstlane((int)((j * kRowsAtOnce + my_row) / RUN));
-        const uint64_t here = ~from.hidden >> (run * RUN % 64u) & (RUN == 64u ? ~0ull : (1ull << (RUN % 64u)) - 1ull);      // any of its tokens that is there names the page
-        const uint32_t of = (uint32_t)__builtin_amdgcn_readlane((int)from.page, (int)(run * RUN + (here ? (uint32_t)__builtin_ctzll(here) : 0u)));
-        const uint32_t in_run = kRowsAtOnce < RUN ? j * kRowsAtOnce % RUN : 0u;
-        x[j] = *reinterpret_cast<const u32x4*>(pool + ((uint64_t)of * a.p.page_stride + (uint64_t)(((uint32_t)t + run * RUN) & in_page) * a.p.token_stride +
-                                                       in_run * a.p.token_stride) + own);
-      }
-    }
-  };
-  const auto careful = [&](uint32_t i, uint64_t lost) { return !whole(tile_at(i), base, reach - 1) || lost != 0ull; };
-  const auto store_keys = [&](uint32_t side) {
-#pragma unroll
-    for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(k_place[side] + key_at<D>(j * kRowsAtOnce + my_row, my_chunk)) = kx[j];
-  };
-  const auto store_values = [&](uint32_t i, const Source& from, uint32_t side) {
-    if (careful(i, from.lost)) {                                       // only there can a value meet a weight that has to be nothing
-#pragma unroll
-      for (uint32_t j = 0; j < kLoads; ++j) {
-        if (from.hidden >> (j * kRowsAtOnce + my_row) & 1ull) vx[j] = (u32x4)(0u);
+        if (!seen_by_some(tile_at(i) + (int32_t)of) || (any_lost && (lost >> of & 1ull))) vx[j] = (u32x4)(0u);
         if (take_out<T>(vx[j])) taken_out = 1u;
       }
-      if (from.lost != 0ull && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
+      if (any_lost && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
     }
 #pragma unroll
-    for (uint32_t j = 0; j < kLoads; ++j)
-      *reinterpret_cast<u32x4*>(v_place[side] + value_at<D>(j * kRowsAtOnce + my_row, my_chunk / 4u) + (my_chunk % 4u) * 16u) = vx[j];
+    for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(v_rows + at + j * kRowsAtOnce * value_row(D)) = vx[j];
   };
-  const auto scores = [&](uint32_t side, f32x16 (&s)[2]) {
-    s[0] = s[1] = (f32x16)(0.0f);
+
+  // The pieces of the work on 32 keys, written out in the order in which they are to be issued: the matrix instructions with what the vector
+  // unit does meanwhile, and the reads of LDS kAhead matrix instructions in front of their use, from the keys on into the values and from the
+  // values on into the next keys.
+  constexpr uint32_t kProducts = 2u * kSlabs, kAhead = D == 64 ? 4u : 6u;
+  static_assert(kAhead <= kSteps && kAhead <= kProducts && kProducts == kSteps);
+  typename T::x8 k_piece[kSteps], v_piece[kProducts];
+  const auto read_key = [&](const uint8_t* at, uint32_t k) { k_piece[k] = __builtin_bit_cast(typename T::x8, *reinterpret_cast<const u32x4*>(at + n * key_row(D) + (k * 2u + h) * 16u)); };
+  const auto read_ahead = [&](const uint8_t* at) {
 #pragma unroll
-    for (uint32_t k = 0; k < kSteps; ++k)
-#pragma unroll
-      for (uint32_t u = 0; u < 2u; ++u) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(k_place[side] + key_at<D>(u * 32u + n, k * 2u + h));
-        s[u] = T::mfma32(__builtin_bit_cast(typename T::x8, x), q[k], s[u]);
-      }
+    for (uint32_t k = 0; k < kAhead; ++k) read_key(at, k);
   };
-  const auto mask = [&](uint32_t i, uint64_t lost, f32x16 (&s)[2]) {
-    const int32_t t = tile_at(i);
-    const int32_t up = mine - t - 4 * (int32_t)h, low = window != 0 ? up - window : -1 - 4 * (int32_t)h - (int32_t)kKeys, sink = window != 0 ? sinks - t - 4 * (int32_t)h : 0;
-#pragma unroll
-    for (uint32_t u = 0; u < 2u; ++u)
-#pragma unroll
-      for (uint32_t j = 0; j < 16u; ++j) {
-        const int32_t c = (int32_t)(u * 32u + 8u * (j / 4u) + j % 4u);
-        bool seen = c <= up && (c > low || c < sink);
-        if ((uint32_t)(lost >> (32u * u)) >> (8u * (j / 4u) + j % 4u + 4u * h) & 1u) seen = false;
-        s[u][j] = seen ? s[u][j] : -INFINITY;
-      }
+  const auto read_value = [&](const uint8_t* at, uint32_t k) {
+    const uint8_t* p = at + (4u * h + (lane % 16u) / 4u) * value_row(D) + (lane / 16u % 2u) * 32u + (lane % 4u) * 8u;
+    const u32x2 lo = read_turned(p + (k / kSlabs) * 16u * value_row(D) + (k % kSlabs) * 64u), hi = read_turned(p + ((k / kSlabs) * 16u + 8u) * value_row(D) + (k % kSlabs) * 64u);
+    v_piece[k] = __builtin_bit_cast(typename T::x8, (u32x4){lo.x, lo.y, hi.x, hi.y});
   };
-  const auto largest = [&](const f32x16 (&s)[2]) {
-    float top = s[0][0];
+  constexpr uint32_t kEach = 16u / kSteps;                             // scores to a matrix instruction
+  typename T::x8 w[2];
+  const auto weigh = [&](const f32x16& s, uint32_t first, uint32_t count) {
+    float e[16], sum = 0.0f;
 #pragma unroll
-    for (uint32_t j = 1; j < 32u; ++j) top = fmaxf(top, s[j / 16u][j % 16u]);
-    return max32(top) * a.scale_log2;
+    for (uint32_t j = first; j < first + count; ++j) e[j] = exp2f_(__builtin_fmaf(s[j], a.scale_log2, -less));
+#pragma unroll
+    for (uint32_t j = first; j < first + count; ++j) {
+      asm volatile("" : "+v"(e[j]));                                   // here, and not behind the next branch
+      sum = j == first ? e[j] : sum + e[j];
+      w[j / 8u][j % 8u] = (typename T::one)e[j];
+    }
+    l += sum;
   };
-  const auto follow = [&](float top) {                                 // m, which is -inf at first, to the largest score there is
-    if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0ull) {
-      const float next = fmaxf(m, top);
+  float top = 0.0f;
+  const auto largest = [&](const f32x16& s, uint32_t first, uint32_t count) {
+#pragma unroll
+    for (uint32_t j = first; j < first + count; ++j) top = j == 0u ? s[0] : fmaxf(top, s[j]);
+  };
+  // scores of 32 keys, whose first pieces have been read, beside the weights of the scores `now`
+  const auto scores = [&](const uint8_t* k_at, const uint8_t* v_at, f32x16& next, const f32x16& now) {
+    next = (f32x16)(0.0f);
+#pragma unroll
+    for (uint32_t k = 0; k < kSteps; ++k) {
+      if (k + kAhead < kSteps) read_key(k_at, k + kAhead);
+      else read_value(v_at, k + kAhead - kSteps);
+      next = T::mfma32(k_piece[k], q[k], next);
+      weigh(now, k * kEach, kEach);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // the product of 32 weights with their values, beside the largest of the scores `next`
+  const auto product = [&](const uint8_t* v_at, const uint8_t* k_next, const f32x16& next) {          // k_next: read with two halves to a tile only
+#pragma unroll
+    for (uint32_t k = 0; k < kProducts; ++k) {
+      if (k + kAhead < kProducts) read_value(v_at, k + kAhead);
+      else if constexpr (kHalves == 2u) read_key(k_next, k + kAhead - kProducts);
+      acc[k % kSlabs] = T::mfma32(v_piece[k], w[k / kSlabs], acc[k % kSlabs]);
+      largest(next, k * kEach, kEach);
+      asm volatile("" : "+v"(top));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const auto mask = [&](uint32_t i, uint32_t half, f32x16& s) {
+    const int32_t t = tile_at(i) + (int32_t)(half * 32u);
+    const int32_t up = mine - t - 4 * (int32_t)h, low = window != 0 ? up - window : -1 - 4 * (int32_t)h - 32, sink = window != 0 ? sinks - t - 4 * (int32_t)h : 0;
+    uint32_t gone = 0u;
+    if (any_lost) {
+      lost = 0ull;
+      settle(i, look_up(i));
+      gone = (uint32_t)(lost >> (32u * half));
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < 16u; ++j) {
+      const int32_t k = (int32_t)(8u * (j / 4u) + j % 4u);
+      bool seen = k <= up && (k > low || k < sink);
+      if (gone >> (8u * (j / 4u) + j % 4u + 4u * h) & 1u) seen = false;
+      s[j] = seen ? s[j] : -INFINITY;
+    }
+  };
+  const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || any_lost; };
+  // m, which is -inf at first, to the largest score there is
+  const auto follow = [&]() {
+    const float most = max32(top) * a.scale_log2;
+    if (__builtin_amdgcn_ballot_w64(most > m + kSlack) != 0ull) {
+      const float next = fmaxf(m, most);
       const float shrink = m == -INFINITY ? 0.0f : exp2f_(m - next);
       l *= shrink;
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d) acc[d] *= shrink;
       m = next;
+      less = m == -INFINITY ? 0.0f : m - kLift;
     }
   };
-  const auto masked = [&](uint32_t i, uint64_t lost) { return !whole(tile_at(i), wave_lo, wave_hi) || lost != 0ull; };
-  const auto weights = [&](const f32x16 (&s)[2], typename T::x8 (&w)[4]) {
-    const float less = m == -INFINITY ? 0.0f : m - kLift;
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) {
-      float e[8];
-#pragma unroll
-      for (uint32_t j = 0; j < 8u; ++j) {
-        e[j] = exp2f_(__builtin_fmaf(s[u / 2u][8u * (u % 2u) + j], a.scale_log2, -less));
-        w[u][j] = (typename T::one)e[j];
-      }
-      l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
-    }
-  };
-  const auto product = [&](uint32_t side, const typename T::x8 (&w)[4]) {
-#pragma unroll
-    for (uint32_t u = 0; u < 4u; ++u) {
-      const uint32_t r = u * 16u + 4u * h + (lane % 16u) / 4u;         // token of the first four
-#pragma unroll
-      for (uint32_t d = 0; d < kSlabs; ++d) {
-        const uint32_t in_piece = (lane / 16u % 2u) * 32u + (lane % 4u) * 8u;
-        const u32x2 lo = read_turned(v_place[side] + value_at<D>(r, d) + in_piece);
-        const u32x2 hi = read_turned(v_place[side] + value_at<D>(r + 8u, d) + in_piece);
-        acc[d] = T::mfma32(__builtin_bit_cast(typename T::x8, (u32x4){lo.x, lo.y, hi.x, hi.y}), w[u], acc[d]);
-      }
-    }
-  };
+
   if (threadIdx.x == 0u) taken_out = 0u;
   __syncthreads();
   if (first_tile < last_tile) {
-    f32x16 s_one[2], s_two[2];
-    typename T::x8 w[4];
-    Source first = {}, second = {}, third = {};                        // of the tiles i + 1, i + 2, i + 3
-    uint32_t i = first_tile, entry = 0u;
-    {
-      const Source from = settle(i, look_up(i));
-      load(keys, i, from, kx);
-      load(values, i, from, vx);
-      if (i + 1u < last_tile) first = settle(i + 1u, look_up(i + 1u));
-      if (i + 2u < last_tile) second = settle(i + 2u, look_up(i + 2u));
-      if (i + 3u < last_tile) entry = look_up(i + 3u);
-      store_keys(0u);
-      store_values(i, from, 0u);
-      if (i + 1u < last_tile) {
-        load(keys, i + 1u, first, kx);
-        load(values, i + 1u, first, vx);
-        store_keys(1u);
-      }
-      if (i + 2u < last_tile) load(keys, i + 2u, second, kx);
-      __syncthreads();
-      scores(0u, s_one);
-      if (masked(i, from.lost)) mask(i, from.lost, s_one);
-      follow(largest(s_one));
-      __syncthreads();
+    constexpr uint32_t kKeyPlace = kKeys * key_row(D), kValuePlace = kKeys * value_row(D);
+    f32x16 s_one, s_two;
+    uint32_t i = first_tile;
+    const auto no_further = [&](uint32_t at) { return min(at, last_tile - 1u); };       // what is read ahead behind the last tile is the last tile
+    uint32_t k_now = 0u, k_next = kKeyPlace, k_free = (kPlaces - 1u) * kKeyPlace, v_now = 0u;      // with two places of K k_free is not used
+    const uint32_t entries_ahead[3] = {look_up(i), look_up(no_further(i + 1u)), look_up(no_further(i + 2u))};
+    uint32_t entry = look_up(no_further(i + 3u));
+    u32x4 second[kLoads];
+    Spots spots = settle(i, entries_ahead[0]);
+    load(keys, spots, kx);
+    load(values, spots, vx);
+    spots = settle(no_further(i + 1u), entries_ahead[1]);
+    load(keys, spots, second);
+    store_keys(0u, kx);
+    store_values(i, 0u);
+    store_keys(kKeyPlace, second);
+    load(values, spots, vx);
+    spots = settle(no_further(i + 2u), entries_ahead[2]);
+    load(keys, spots, kx);
+    __syncthreads();
+    s_one = (f32x16)(0.0f);
+#pragma unroll
+    for (uint32_t k = 0; k < kSteps; ++k) {
+      read_key(k_place[0], k);
+      s_one = T::mfma32(k_piece[k], q[k], s_one);
     }
-    // One tile: its weights and its product with the values, with the next tile's scores and their maximum.
-    const auto step = [&](uint32_t side, const f32x16 (&now)[2], f32x16 (&next)[2]) {
-      // keys of i + 2 take the place of those of i, values of i + 1 that of those of i - 1
-      if (i + 2u < last_tile) store_keys(side);
-      store_values(i + 1u, first, side ^ 1u);
-      if (i + 3u < last_tile) {
-        third = settle(i + 3u, entry);
-        load(keys, i + 3u, third, kx);
-      }
-      if (i + 2u < last_tile) load(values, i + 2u, second, vx);
-      if (i + 4u < last_tile) entry = look_up(i + 4u);
-      scores(side ^ 1u, next);
-      weights(now, w);
-      if (masked(i + 1u, first.lost)) mask(i + 1u, first.lost, next);
-      product(side, w);
-      follow(largest(next));
-      first = second;
-      second = third;
-      ++i;
-      __syncthreads();
+    if (masked(i)) mask(i, 0u, s_one);
+    largest(s_one, 0u, 16u);
+    follow();
+    if constexpr (kHalves == 2u) read_ahead(k_place[0] + 32u * key_row(D));
+    __syncthreads();
+    // 32 keys: the weights of `now` and their product with the values, beside the scores of the next 32 and their largest.
+    const auto half = [&](const uint8_t* k_at, const uint8_t* v_at, const uint8_t* k_next, const f32x16& now, f32x16& next, uint32_t next_tile, uint32_t next_half) {
+      scores(k_at, v_at, next, now);
+      if (masked(next_tile)) mask(next_tile, next_half, next);
+      product(v_at, k_next, next);
+      follow();
     };
-    while (i + 2u < last_tile) {
-      step(0u, s_one, s_two);
-      step(1u, s_two, s_one);
+    const auto last_half = [&](const uint8_t* v_at, const f32x16& now) {
+      weigh(now, 0u, 16u);
+#pragma unroll
+      for (uint32_t k = 0; k < kProducts; ++k) {
+        read_value(v_at, k);
+        acc[k % kSlabs] = T::mfma32(v_piece[k], w[k / kSlabs], acc[k % kSlabs]);
+      }
+    };
+    for (; i + 1u < last_tile; ++i) {
+      // the keys of tile i + 2 and the values of i + 1 take places that nobody reads any more; those of i + 3 and i + 2 are asked for
+      store_keys(kHalves == 2u ? k_free : k_now, kx);
+      store_values(i + 1u, kValuePlace - v_now);
+      load(values, spots, vx);
+      spots = settle(no_further(i + 3u), entry);
+      load(keys, spots, kx);
+      entry = look_up(no_further(i + 4u));
+      const uint8_t *const v_at = v_place[0] + v_now, *const k_at = k_place[0] + k_now, *const k_then = k_place[0] + k_next;
+      if constexpr (kHalves == 2u) {
+        half(k_at + 32u * key_row(D), v_at, k_then, s_one, s_two, i, 1u);
+        half(k_then, v_at + 32u * value_row(D), k_then + 32u * key_row(D), s_two, s_one, i + 1u, 0u);
+        const uint32_t old = k_now;
+        k_now = k_next;
+        k_next = k_free;
+        k_free = old;
+      } else {
+        read_ahead(k_then);                                            // the tile after it takes its place meanwhile, behind the barrier
+        half(k_then, v_at, k_then, s_one, s_two, i + 1u, 0u);
+        s_one = s_two;
+        k_now = k_next;
+        k_next = kKeyPlace - k_next;
+      }
+      v_now = kValuePlace - v_now;
+      __syncthreads();
     }
-    if (i + 1u < last_tile) {
-      step(0u, s_one, s_two);
-      weights(s_two, w);
-      product(1u, w);
+    const uint8_t *const v_at = v_place[0] + v_now, *const k_at = k_place[0] + k_now;
+    if constexpr (kHalves == 2u) {
+      half(k_at + 32u * key_row(D), v_at, k_at, s_one, s_two, i, 1u);
+      last_half(v_at + 32u * value_row(D), s_two);
     } else {
-      weights(s_one, w);
-      product(0u, w);
+      last_half(v_at, s_one);
     }
   }
 
-  if (taken_out != 0u && live) {
-    // What was taken out counts for the pairs that see it, and for no other: their sums become infinite or no number, whatever the weight.
-    for (uint32_t i = first_tile; i < last_tile; ++i) {
-      const int32_t t = tile_at(i);
-      for (int32_t key = t; key < t + (int32_t)kKeys; ++key) {
-        if (key > mine || key >= reach || (window != 0 && key <= mine - window && key >= sinks)) continue;
-        const uint32_t page = (uint32_t)entries[(uint32_t)key >> a.p.page_shift];
-        if (page >= a.p.pages) continue;
-        const uint8_t* from = values + (uint64_t)page * a.p.page_stride + (uint64_t)((uint32_t)key & in_page) * a.p.token_stride + h * 8u;
+  if (live) {
+    if (taken_out != 0u) {
+      // What was taken out counts for the pairs that see it, and for no other: their sums become infinite or no number, whatever the weight.
+      for (uint32_t i = first_tile; i < last_tile; ++i) {
+        const int32_t t = tile_at(i);
+        for (int32_t key = t; key < t + (int32_t)kKeys; ++key) {
+          if (key > mine || key >= reach || (window != 0 && key <= mine - window && key >= sinks)) continue;
+          const uint32_t page = (uint32_t)entries[(uint32_t)key >> a.p.page_shift];
+          if (page >= a.p.pages) continue;
+          const uint8_t* from = values + (uint64_t)page * a.p.page_stride + (uint64_t)((uint32_t)key & in_page) * a.p.token_stride + h * 8u;
 #pragma unroll
-        for (uint32_t d = 0; d < kSlabs; ++d)
+          for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
-          for (uint32_t j = 0; j < 4u; ++j) {
-            const typename T::x4 v = *reinterpret_cast<const typename T::x4*>(from + (d * 4u + j) * 16u);
+            for (uint32_t j = 0; j < 4u; ++j) {
+              const typename T::x4 v = *reinterpret_cast<const typename T::x4*>(from + (d * 4u + j) * 16u);
 #pragma unroll
-            for (uint32_t e = 0; e < 4u; ++e)
-              if (!(__builtin_fabsf((float)v[e]) < INFINITY)) acc[d][4u * j + e] += (float)v[e];
-          }
+              for (uint32_t e = 0; e < 4u; ++e)
+                if (!(__builtin_fabsf((float)v[e]) < INFINITY)) acc[d][4u * j + e] += (float)v[e];
+            }
+        }
       }
     }
-  }
-  if (!live) return;
-  l = sum32(l);
-  const uint64_t out = query * q_heads + hq;
-  if constexpr (SPLIT) {
-    const uint64_t slot = (uint64_t)blockIdx.y * a.tokens * q_heads + out;
+    const uint64_t out_at = query * q_heads + hq;
+    const float sum = sum32(l);
+    if constexpr (SPLIT) {
+      const uint64_t slot = (uint64_t)blockIdx.y * a.tokens * q_heads + out_at;
 #pragma unroll
-    for (uint32_t d = 0; d < kSlabs; ++d)
+      for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
-      for (uint32_t j = 0; j < 4u; ++j)
-        *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32u + j * 8u + h * 4u) = (f32x4){acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]};
-    if (h == 0u) *reinterpret_cast<f32x2*>(a.part_ml + slot * 2u) = (f32x2){m, l};
-  } else {
-    const float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+        for (uint32_t j = 0; j < 4u; ++j)
+          *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32u + j * 8u + h * 4u) = (f32x4){acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]};
+      if (h == 0u) *reinterpret_cast<f32x2*>(a.part_ml + slot * 2u) = (f32x2){m, sum};
+    } else {
+      const float scale = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
 #pragma unroll
-    for (uint32_t d = 0; d < kSlabs; ++d)
+      for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
-      for (uint32_t j = 0; j < 4u; ++j) {
-        typename T::x4 o;
+        for (uint32_t j = 0; j < 4u; ++j) {
+          typename T::x4 o;
 #pragma unroll
-        for (uint32_t e = 0; e < 4u; ++e) o[e] = (typename T::one)(acc[d][4u * j + e] * scale);
-        *reinterpret_cast<typename T::x4*>(a.out + (out * D + d * 32u + j * 8u + h * 4u) * 2u) = o;
-      }
-    if (a.lse && h == 0u) a.lse[out] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(l)) * 0.6931471805599453f;
+          for (uint32_t e = 0; e < 4u; ++e) o[e] = (typename T::one)(acc[d][4u * j + e] * scale);
+          *reinterpret_cast<typename T::x4*>(a.out + (out_at * D + d * 32u + j * 8u + h * 4u) * 2u) = o;
+        }
+      if (a.lse && h == 0u) a.lse[out_at] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(sum)) * 0.6931471805599453f;
+    }
   }
 }
 
@@ -366,16 +435,33 @@ __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptAr
   const uint32_t at = threadIdx.x % kLanes;
   const uint32_t used = (uint32_t)a.starts[a.p.rows];                  // tokens behind the last sequence have no parts
   if (pair >= all || pair / (a.p.kv_heads * a.rep) >= used || pair / (a.p.kv_heads * a.rep) < (uint32_t)a.starts[0]) return;
+  constexpr uint32_t kAtOnce = 8;
   float m = -INFINITY, l = 0.0f;
   f32x4 o = (f32x4)(0.0f);
-  for (uint32_t s = 0; s < a.splits; ++s) {
-    const uint64_t slot = s * all + pair;
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
-    const float top = fmaxf(m, ml.x);
-    const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top), take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);
-    l = l * keep + ml.y * take;
-    o = o * keep + x * take;
+  for (uint32_t s = 0; s < a.splits; s += kAtOnce) {
+    f32x2 ml[kAtOnce];
+    f32x4 x[kAtOnce];
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const uint64_t slot = min(s + k, a.splits - 1u) * all + pair;    // past the last one: the last one, without weight
+      ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
+      x[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
+    }
+    float top = m;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      if (s + k >= a.splits) ml[k].x = -INFINITY;
+      top = fmaxf(top, ml[k].x);
+    }
+    const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top);
+    l *= keep;
+    o *= keep;
+#pragma unroll
+    for (uint32_t k = 0; k < kAtOnce; ++k) {
+      const float take = ml[k].x == -INFINITY ? 0.0f : exp2f_(ml[k].x - top);
+      l += ml[k].y * take;
+      o += x[k] * take;
+    }
     m = top;
   }
   const float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
@@ -394,14 +480,21 @@ void launch_prompt_run(const PagedPromptArgs& a, hipStream_t stream) {
   else prompt_kernel<T, D, 1u, SPLIT, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
 }
 
+template <typename T, int D, bool SPLIT>
+void launch_prompt_waves(const PagedPromptArgs& a, hipStream_t stream) {
+  if constexpr (D != 256) {
+    if (a.waves == 8u) return launch_prompt_run<T, D, SPLIT, 8u>(a, stream);
+  }
+  launch_prompt_run<T, D, SPLIT, 4u>(a, stream);
+}
+
 template <typename T, int D>
 hipError_t launch_prompt_of(const PagedPromptArgs& a, hipStream_t stream) {
   if (a.splits == 1u) {
-    if (D <= 128 && a.waves == 8u) launch_prompt_run<T, D <= 128 ? D : 64, false, 8u>(a, stream);
-    else launch_prompt_run<T, D, false, 4u>(a, stream);
+    launch_prompt_waves<T, D, false>(a, stream);
     return hipGetLastError();
   }
-  launch_prompt_run<T, D, true, 4u>(a, stream);
+  launch_prompt_waves<T, D, true>(a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const uint64_t pairs = (uint64_t)a.tokens * (a.p.kv_heads * a.rep);
