@@ -63,18 +63,21 @@ QKV_HD TileRange tile_range(const Seen& s, uint32_t i) {
   return t;
 }
 
-// `total` tiles dealt to shares in a row, the first ones one more than the last ones.
+// `total` tiles dealt to at most `most` shares in a row: kAttendLeast each while that is enough, otherwise in equal parts, the first ones one more than the
+// last ones.
 struct Shares {
-  uint32_t shares, each, more;       // share i has each + (i < more) tiles
+  uint32_t shares, each, more, total;      // share i has each + (i < more) tiles
 };
 QKV_HD Shares deal(uint32_t total, uint32_t most) {
-  uint32_t n = (total + kAttendLeast - 1u) / kAttendLeast;
-  if (n > most) n = most;
-  if (n < 1u) n = 1u;
-  return Shares{n, total / n, total % n};
+  if (total <= kAttendLeast * most) return Shares{(total + kAttendLeast - 1u) / kAttendLeast, kAttendLeast, 0u, total};
+  return Shares{most, total / most, total % most, total};
 }
-QKV_HD uint32_t share_begin(const Shares& s, uint32_t i) { return i * s.each + (i < s.more ? i : s.more); }
+QKV_HD uint32_t share_begin(const Shares& s, uint32_t i) {
+  const uint32_t at = i * s.each + (i < s.more ? i : s.more);
+  return at < s.total ? at : s.total;
+}
 QKV_HD uint32_t share_of(const Shares& s, uint32_t tile) {
+  if (s.more == 0u && s.each == kAttendLeast) return tile / kAttendLeast;
   const uint32_t big = s.more * (s.each + 1u);
   return tile < big ? tile / (s.each + 1u) : s.more + (tile - big) / s.each;
 }
@@ -126,7 +129,8 @@ struct PagedAttendArgs {
   uint64_t q_token_stride, q_head_stride;                // bytes
   uint32_t rep, blocks;                                  // query heads per kv head, groups of 16 of them
   uint32_t window, sinks;
-  float scale_log2;                                      // softmax scale times log2(e)
+  float scale_log2;                                      // softmax scale times log2(e), never 0
+  float nothing;                                         // a score that weighs nothing: -inf, or +inf where the scale is negative
   const float *prior_out, *prior_lse;
   float *out, *lse;
   float *part_o, *part_ml;                               // [items + most shares][heads of a block][dim], [...][2]

@@ -96,6 +96,12 @@ uint64_t most_tiles(const qkv_pages_t* p) { return ((uint64_t)p->row_pages * (ui
 // A window that holds any sequence the table has room for is none.
 uint32_t window_of(const qkv_pages_t* p, int32_t window) { return (int64_t)window >= (int64_t)p->row_pages * p->page_tokens ? 0u : (uint32_t)window; }
 
+// The scale for powers of two.  One of 0 is as good as none, but infinity times it has to stay infinite.
+float scale_of(float scale) {
+  const float x = (float)((double)scale * 1.4426950408889634);
+  return std::fabs(x) >= 1e-37f ? x : x < 0.0f ? -1e-37f : 1e-37f;
+}
+
 struct AttendPlan {
   uint32_t rep, blocks, heads;      // query heads per kv head, groups of 16, heads of a group
   uint64_t items;
@@ -256,7 +262,8 @@ int qkv_paged_attend(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   a.blocks = plan.blocks;
   a.window = window_of(pages, query->window);
   a.sinks = a.window ? (uint32_t)query->sinks : 0u;
-  a.scale_log2 = (float)((double)query->softmax_scale * 1.4426950408889634);
+  a.scale_log2 = scale_of(query->softmax_scale);
+  a.nothing = a.scale_log2 < 0.0f ? INFINITY : -INFINITY;
   a.prior_out = query->prior_out_dev;
   a.prior_lse = query->prior_lse_dev;
   a.out = static_cast<float*>(query->out_dev);
@@ -307,8 +314,7 @@ int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   a.waves = plan.waves;
   a.window = window_of(pages, query->window);
   a.sinks = a.window ? (uint32_t)query->sinks : 0u;
-  a.scale_log2 = (float)(std::fabs((double)query->softmax_scale) * 1.4426950408889634);
-  if (!(a.scale_log2 >= 1e-37f)) a.scale_log2 = 1e-37f;        // 0: all scores equal, and -inf stays -inf
+  a.scale_log2 = std::fabs(scale_of(query->softmax_scale));
   a.flip = query->softmax_scale < 0.0f ? 1u : 0u;
   a.out = static_cast<uint8_t*>(query->out_dev);
   a.lse = query->lse_dev;

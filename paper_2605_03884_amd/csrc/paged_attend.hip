@@ -14,6 +14,7 @@
 //   values   O^T = V^T P^T: the weights are already where the product wants them (a lane's 8 tokens, in an order of the tokens that V
 //            follows); V^T wants 4 tokens of one dimension in a lane, which the transposing read of LDS gives.
 //            Rows of V stand in LDS with their 32-byte pieces exchanged by token, so that neither side meets a bank twice.
+// The sum of a head that sees anything is at least 2^10, so the hardware's reciprocal and logarithm, which know no subnormals, serve (1 step each).
 // The weights are held to 22 bits (fp16: high part and remainder; bf16, 8 bits each, high part and two remainders), scaled by 2^10 so that
 // what fp16 loses below 2^-14 counts for nothing; maxima, sums and results are in 32 bits.
 #include <algorithm>
@@ -50,8 +51,8 @@ __device__ inline Lengths read_lengths(const PagedAttendArgs& a, uint32_t lane) 
   return n;
 }
 
-// The row that tile `at` of all rows falls into, the tiles in front of that row, and its length.
-__device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, const Lengths& n, uint32_t lane, uint32_t at, uint32_t& before, uint32_t& length) {
+// The row that tile `at` of all items falls into, the tiles in front of that row, and its length.  `inner`: items of a row.
+__device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, const Lengths& n, uint32_t lane, uint32_t inner, uint32_t at, uint32_t& before, uint32_t& length) {
   before = 0u;
   for (uint32_t base = 0;; base += kWaveSize) {
     const uint32_t row = base + lane;
@@ -60,6 +61,7 @@ __device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, const Lengths& 
       here = row < a.p.rows ? row_length(a, row) : 0u;
       mine = row < a.p.rows ? seen_tiles(seen_by_last(here, a.window, a.sinks)) : 0u;
     }
+    mine *= inner;
     const uint32_t upto = before + wave_inclusive_scan(mine);
     const uint64_t over = __builtin_amdgcn_ballot_w64(upto > at);
     if (over != 0ull || base + kWaveSize >= a.p.rows) {
@@ -148,15 +150,22 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
   uint32_t at = share_begin(shares, share);
   const uint32_t end = share_begin(shares, share + 1u);
   uint32_t before, length;
-  uint32_t row = row_of_tile(a, lengths, lane, at / inner_count, before, length);
+  uint32_t row = row_of_tile(a, lengths, lane, inner_count, at, before, length);
   Seen seen = seen_by_last(length, a.window, a.sinks);
   uint32_t tiles = seen_tiles(seen);
-  uint32_t inner = (at - before * inner_count) / tiles, tile = (at - before * inner_count) % tiles;
+  // the item of the row, by counting those that end in front of `at`: a division took longer
+  uint32_t inner = 0u;
+  for (uint32_t base = 0; base < inner_count; base += kWaveSize) {
+    const uint64_t ended = __builtin_amdgcn_ballot_w64(base + lane < inner_count && before + (base + lane + 1u) * tiles <= at);
+    inner += (uint32_t)__builtin_popcountll(ended);
+    if (ended != ~0ull) break;
+  }
+  uint32_t tile = at - before - inner * tiles;
   uint8_t* mine = lds[wave];
 
   while (at < end) {
     // one item, or what of it falls into this share
-    const uint32_t head = inner / a.blocks, block = inner % a.blocks;
+    const uint32_t head = a.blocks == 1u ? inner : inner / a.blocks, block = a.blocks == 1u ? 0u : inner % a.blocks;
     const uint32_t heads = min(16u, a.rep - block * 16u);
     const uint32_t from = tile, upto = min(tiles, tile + (end - at));
     const uint32_t hq = head * a.rep + block * 16u + n;                // this lane's query head, if n < heads
@@ -215,22 +224,17 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
           entry = look_up<RUN>(a, row, range, lane);
         }
       }
-      float e[8];
-      float top = -INFINITY;
-      if (counted == 0xFFFFFFFFu) {
+      if (counted != 0xFFFFFFFFu) {                                    // what does not count scores -inf, and its values, whatever they are, are 0
 #pragma unroll
-        for (uint32_t j = 0; j < 8u; ++j) {
-          e[j] = s[j / 4u][j % 4u];
-          top = fmaxf(top, e[j] * a.scale_log2);
-        }
-      } else {
+        for (uint32_t j = 0; j < 8u; ++j)
+          s[j / 4u][j % 4u] = (counted >> (16u * (j / 4u) + 4u * g + j % 4u)) & 1u ? s[j / 4u][j % 4u] : a.nothing;
 #pragma unroll
-        for (uint32_t j = 0; j < 8u; ++j) {
-          e[j] = s[j / 4u][j % 4u];
-          const float x = (counted >> (16u * (j / 4u) + 4u * g + j % 4u)) & 1u ? e[j] * a.scale_log2 : -INFINITY;
-          top = fmaxf(top, x);
-        }
+        for (uint32_t j = 0; j < kLoads; ++j) vx[j] = (counted >> (j * kRowsAtOnce + lane / kRowLanes)) & 1u ? vx[j] : (u32x4)(0u);
       }
+      float e[8];
+      float top = s[0][0] * a.scale_log2;
+#pragma unroll
+      for (uint32_t j = 1; j < 8u; ++j) top = fmaxf(top, s[j / 4u][j % 4u] * a.scale_log2);
       top = max32(max16(top));
       const float m_new = fmaxf(m, top);
       const float less = m_new == -INFINITY ? 0.0f : m_new - kLift;    // what is taken off in the exponent
@@ -241,19 +245,8 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
         for (uint32_t d = 0; d < kSlabs; ++d) acc[d] *= shrink;
         m = m_new;
       }
-      if (counted == 0xFFFFFFFFu) {
 #pragma unroll
-        for (uint32_t j = 0; j < 8u; ++j) e[j] = exp2f_(__builtin_fmaf(e[j], a.scale_log2, -less));
-      } else {
-#pragma unroll
-        for (uint32_t j = 0; j < 8u; ++j)
-          e[j] = (counted >> (16u * (j / 4u) + 4u * g + j % 4u)) & 1u ? exp2f_(__builtin_fmaf(e[j], a.scale_log2, -less)) : 0.0f;
-#pragma unroll
-        for (uint32_t j = 0; j < kLoads; ++j) {                        // whatever stands in rows that do not count
-          const bool counts = (counted >> (j * kRowsAtOnce + lane / kRowLanes)) & 1u;
-          vx[j] = counts ? vx[j] : (u32x4)(0u);
-        }
-      }
+      for (uint32_t j = 0; j < 8u; ++j) e[j] = exp2f_(__builtin_fmaf(s[j / 4u][j % 4u], a.scale_log2, -less));
       l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       typename T::x8 w[T::kParts];
       T::parts(e, w);
@@ -282,8 +275,8 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
     l = sum32(sum16(l));
     if (from == 0u && upto == tiles) {                                 // the whole item
       const uint64_t at_head = (uint64_t)row * q_heads + hq;
-      float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-      float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(l)) * 0.6931471805599453f;
+      float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+      float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
       float other = 0.0f;
       if (n < heads) {
         if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
@@ -383,8 +376,8 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a,
     m = top;
   }
   const uint64_t at_head = (uint64_t)row * q_heads + (inner / a.blocks) * a.rep + block * 16u + in_block;
-  float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-  float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(l)) * 0.6931471805599453f;
+  float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+  float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   float other = 0.0f;
   if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
   o *= scale;

@@ -260,22 +260,20 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // what the lane's pair does not see of 32 keys scores -inf: a bit for each key
   const auto mask = [&](uint32_t i, uint32_t half, f32x16& s) {
     const int32_t t = tile_at(i) + (int32_t)(half * 32u);
-    const int32_t up = mine - t - 4 * (int32_t)h, low = window != 0 ? up - window : -1 - 4 * (int32_t)h - 32, sink = window != 0 ? sinks - t - 4 * (int32_t)h : 0;
-    uint32_t gone = 0u;
+    const auto below = [](int32_t n) { return (uint32_t)((1ull << (uint32_t)min(max(n, 0), 32)) - 1ull); };
+    uint32_t seen = below(mine - t + 1);
+    if (window != 0) seen &= ~below(mine - t - window + 1) | below(sinks - t);
     if (any_lost) {
       lost = 0ull;
       settle(i, look_up(i));
-      gone = (uint32_t)(lost >> (32u * half));
+      seen &= ~(uint32_t)(lost >> (32u * half));
     }
+    seen >>= 4u * h;
 #pragma unroll
-    for (uint32_t j = 0; j < 16u; ++j) {
-      const int32_t k = (int32_t)(8u * (j / 4u) + j % 4u);
-      bool seen = k <= up && (k > low || k < sink);
-      if (gone >> (8u * (j / 4u) + j % 4u + 4u * h) & 1u) seen = false;
-      s[j] = seen ? s[j] : -INFINITY;
-    }
+    for (uint32_t j = 0; j < 16u; ++j) s[j] = seen >> (8u * (j / 4u) + j % 4u) & 1u ? s[j] : -INFINITY;
   };
   const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || any_lost; };
   // m, which is -inf at first, to the largest score there is
@@ -409,7 +407,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
           *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32u + j * 8u + h * 4u) = (f32x4){acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]};
       if (h == 0u) *reinterpret_cast<f32x2*>(a.part_ml + slot * 2u) = (f32x2){m, sum};
     } else {
-      const float scale = sum > 0.0f ? 1.0f / sum : sum == 0.0f ? 0.0f : sum;
+      const float scale = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
@@ -419,7 +417,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
           for (uint32_t e = 0; e < 4u; ++e) o[e] = (typename T::one)(acc[d][4u * j + e] * scale);
           *reinterpret_cast<typename T::x4*>(a.out + (out_at * D + d * 32u + j * 8u + h * 4u) * 2u) = o;
         }
-      if (a.lse && h == 0u) a.lse[out_at] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(sum)) * 0.6931471805599453f;
+      if (a.lse && h == 0u) a.lse[out_at] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     }
   }
 }
@@ -464,12 +462,12 @@ __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptAr
     }
     m = top;
   }
-  const float scale = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+  const float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
   typename T::x4 r;
 #pragma unroll
   for (uint32_t e = 0; e < 4u; ++e) r[e] = (typename T::one)(o[e] * scale);
   *reinterpret_cast<typename T::x4*>(a.out + (pair * D + at * 4u) * 2u) = r;
-  if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_log2f(l)) * 0.6931471805599453f;
+  if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, bool SPLIT, uint32_t WAVES>

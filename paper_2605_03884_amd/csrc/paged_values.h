@@ -58,7 +58,7 @@ __device__ inline void join(float& lse, float other_lse, float& scale, float& ot
   const float both = a + b;
   scale *= a / both;
   other = b / both;
-  lse = top + __builtin_log2f(both) * 0.6931471805599453f;
+  lse = top + __builtin_amdgcn_logf(both) * 0.6931471805599453f;       // both: 1 to 2
 }
 
 struct Half {
