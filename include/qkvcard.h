@@ -541,6 +541,7 @@ int qkv_pages_reserve(const qkv_pages_t* pages, const int32_t* more_dev, uint32_
  * Rows of new tokens into the pages of the sequences' last places.  Token i of row b, i = starts_dev[b] .. starts_dev[b + 1] - 1 of the
  * batch, goes to place lens_dev[b] - (starts_dev[b + 1] - starts_dev[b]) + (i - starts_dev[b]): lengths count the new tokens already.
  *   starts_dev: device, int32_t[rows + 1], rising; NULL: one token for every row (tokens == rows), which a row of length 0 leaves out.
+ *   tokens: below 2^27.
  *   k_dev, v_dev: device, the new rows: layer l (counted from layer_begin), token i, head h start l * layer_stride + i * token_stride +
  *             h * head_stride elements behind it; strides multiples of 8, below 2^40, pointers 16-byte aligned.  A dense cache of
  *             qkv_unpack_dequant goes in with layer_stride = H*T*D, head_stride = T*D, token_stride = D.

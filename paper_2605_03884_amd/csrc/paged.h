@@ -94,6 +94,30 @@ QKV_HD uint32_t held(int32_t length, uint32_t row_pages, uint32_t page_shift) {
 QKV_HD uint32_t first_place(uint32_t start, uint32_t b, uint32_t per) { return start / per + b; }
 QKV_HD uint32_t places(uint32_t tokens, uint32_t rows, uint32_t per) { return tokens / per + rows; }
 
+// The keys that the queries at places [base, base + here) see, in tiles of `keys`: those of the sinks, [0, sink_end), are `head` tiles, the others the tiles
+// `body` and on, `tiles` in all.  Nobody sees a key of [sink_end, win_lo).
+struct KeyTiles {
+  int32_t win_lo;
+  uint32_t sink_end, head, body, tiles;
+};
+QKV_HD KeyTiles key_tiles_of(int32_t base, uint32_t here, int32_t window, int32_t sinks, uint32_t keys) {
+  KeyTiles k;
+  const int32_t reach = base + (int32_t)here;
+  k.win_lo = window != 0 && base >= window ? base - window + 1 : 0;
+  k.sink_end = (uint32_t)(sinks < k.win_lo ? sinks : k.win_lo);
+  k.head = (k.sink_end + keys - 1u) / keys;
+  k.body = (uint32_t)k.win_lo / keys;
+  if (k.body < k.head) k.body = k.head;
+  const uint32_t stop = reach > 0 ? ((uint32_t)reach + keys - 1u) / keys : 0u;
+  k.tiles = k.head + (stop > k.body ? stop - k.body : 0u);
+  return k;
+}
+// Parts the keys of a query tile are cut into: as many as there may be, of at least 512 keys.
+QKV_HD uint32_t prompt_splits(uint32_t keys, uint32_t most) {
+  const uint32_t n = keys / 512u;
+  return n < 2u ? 1u : n < most ? n : most;
+}
+
 // One layer of a cache in pages.
 struct PageLayer {
   const uint8_t *k, *v;

@@ -114,7 +114,7 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
   a.blocks = (a.rep + 15u) / 16u;
   a.heads = a.rep < 16u ? a.rep : 16u;
   a.items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
-  if (a.items * most_tiles(p) >= (1ull << 31)) return QKV_ERR_SHAPE;
+  if (a.items * most_tiles(p) >= (1ull << 31) || a.items >= (1ull << 22)) return QKV_ERR_SHAPE;
   a.split = most_tiles(p) - 2u > kAttendLeast;
   // Waves: as many as the chip holds at once at the kernel's registers (64 dimensions: three quarters, 3072 took 32.6 us where 2048 take 32.0),
   // or as many as have 4 tiles each.
@@ -131,17 +131,18 @@ struct PromptPlan {
 int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
   if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
   a.rep = (uint32_t)(q_heads / p->kv_heads);
-  // Tiles of 256 pairs, where the mean sequence has more than 128 of them to a kv head; 256 dimensions have no registers for more than 128.
-  a.waves = p->head_dim <= 128 && tokens * a.rep > 128 * (int64_t)p->rows ? 8u : 4u;
+  // 128 dimensions: tiles of 256 pairs (8 waves) where there is one for every CU (an 8K prompt 566 us, with tiles of 128 626; six short prompts 21.8, 17.5).
+  // 64 dimensions do better with three workgroups of 4 waves a CU (170 us, 198), 256 have no registers for two waves a SIMD.
+  a.waves = p->head_dim == 128 && tokens * q_heads >= 256 * 256 ? 8u : 4u;
   a.per = 32u * a.waves / a.rep;
   const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
-  if (tiles >= (1ull << 31)) return QKV_ERR_SHAPE;
-  // Few query tiles: the keys are split until there is a workgroup of 8 waves or two of 4 to a CU, into shares of at least 512 tokens.  (61 tokens of 32
-  // heads behind 32768: 75 us with 128 workgroups, 67 with 256, 87 with 384.)
-  const uint64_t room = (uint64_t)p->row_pages * (uint64_t)p->page_tokens / 512u;
-  uint64_t n = (a.waves == 8u ? 256u : 512u) / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
+  if (tiles * a.waves * 64u >= (1ull << 32)) return QKV_ERR_SHAPE;       // threads of a grid's dimension
+  // Few query tiles: the keys are split until there are two workgroups to a CU, where sequences turn out to have that many (61 tokens of 32 heads behind
+  // 32768: 16 parts 75 us, 32 65, 64 87 while their join still took a fifth longer).  Tiles of 256 pairs are never so few.
+  const uint64_t room = prompt_splits((uint32_t)p->row_pages * (uint32_t)p->page_tokens + 128u, 64u);
+  uint64_t n = 512u / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
+  if (a.waves == 8u) n = 1u;
   if (n > room) n = room;
-  if (n > 64u) n = 64u;
   a.splits = n < 2u ? 1u : (uint32_t)n;
   a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
   return QKV_OK;
@@ -156,7 +157,7 @@ int qkv_pages_append(const qkv_pages_t* pages, const qkv_rows_t* rows, uint32_t*
   if (rc) return rc;
   if (!rows || !rows->k_dev || !rows->v_dev) return QKV_ERR_NULL;
   if (rows->layer_begin < 0 || rows->layer_count < 1 || rows->layer_begin > pages->layers - rows->layer_count) return QKV_ERR_SHAPE;
-  if (rows->tokens < 0 || rows->tokens >= (1ll << 31) || (!rows->starts_dev && rows->tokens != pages->rows)) return QKV_ERR_SHAPE;
+  if (rows->tokens < 0 || rows->tokens >= (1ll << 27) || (!rows->starts_dev && rows->tokens != pages->rows)) return QKV_ERR_SHAPE;
   const int64_t strides[3] = {rows->layer_stride, rows->head_stride, rows->token_stride};
   for (int i = 0; i < 3; ++i)
     if (strides[i] < 0 || strides[i] % 8 != 0 || strides[i] >= (1ll << 40)) return QKV_ERR_SHAPE;

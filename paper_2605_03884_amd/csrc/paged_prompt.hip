@@ -30,7 +30,7 @@ constexpr float kLift = 7.0f, kSlack = 8.0f;
 // Keys of a tile: as many as leave LDS for two workgroups of 4 waves a CU, or one of 8.
 constexpr uint32_t prompt_keys(uint32_t waves) { return waves == 8u ? 64u : 32u; }
 // Waves a SIMD holds at once: what its 512 registers allow.
-constexpr uint32_t prompt_waves_a_simd(int D) { return D == 256 ? 1u : 2u; }
+constexpr uint32_t prompt_waves_a_simd(int D) { return D == 256 ? 1u : D == 128 ? 2u : 3u; }
 
 constexpr uint32_t key_row(int D) { return D * 2u + 16u; }
 constexpr uint32_t value_row(int D) { return D * 2u + 64u; }
@@ -83,13 +83,13 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   if (base < 0 && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_ROW);
   const int32_t window = (int32_t)a.window, sinks = (int32_t)min(a.sinks, 0x7FFFFFFFu);
   const int32_t reach = base + (int32_t)here;                          // keys below it are seen by somebody
-  const int32_t win_lo = window != 0 && base >= window ? base - window + 1 : 0;
-  const uint32_t sink_end = (uint32_t)min(sinks, win_lo);
-  const uint32_t head = (sink_end + kKeys - 1u) / kKeys;
-  const uint32_t body = max((uint32_t)win_lo / kKeys, head), stop = reach > 0 ? ((uint32_t)reach + kKeys - 1u) / kKeys : 0u;
-  const uint32_t tiles = head + (stop > body ? stop - body : 0u);
-  const uint32_t first_tile = SPLIT ? (uint32_t)((uint64_t)tiles * blockIdx.y / a.splits) : 0u;
-  const uint32_t last_tile = SPLIT ? (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / a.splits) : tiles;
+  const KeyTiles key_tiles = key_tiles_of(base, here, window, sinks, kKeys);
+  const int32_t win_lo = key_tiles.win_lo;
+  const uint32_t sink_end = key_tiles.sink_end, head = key_tiles.head, body = key_tiles.body, tiles = key_tiles.tiles;
+  const uint32_t splits = SPLIT ? prompt_splits(tiles * kKeys, a.splits) : 1u;
+  if (SPLIT && blockIdx.y >= splits) return;
+  const uint32_t first_tile = SPLIT ? (uint32_t)((uint64_t)tiles * blockIdx.y / splits) : 0u;
+  const uint32_t last_tile = SPLIT ? (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / splits) : tiles;
   const auto tile_at = [&](uint32_t i) -> int32_t { return (int32_t)((i < head ? i : body + (i - head)) * kKeys); };
   // Tiles [from, from + count) are seen whole by all queries at places [lo, hi]; those of the sinks are not counted among them.
   struct Range {
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     }
     const uint64_t out_at = query * q_heads + hq;
     const float sum = sum32(l);
-    if constexpr (SPLIT) {
+    if (SPLIT && splits != 1u) {
       const uint64_t slot = (uint64_t)blockIdx.y * a.tokens * q_heads + out_at;
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d)
@@ -422,33 +422,39 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   }
 }
 
-// Joins the parts of every (query token, query head): D / 4 lanes each.
+// Joins the parts of the query heads of one token, D / 4 lanes each.
 constexpr uint32_t kJoinThreads = 256;
 
-template <typename T, int D>
+template <typename T, int D, uint32_t KEYS>
 __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptArgs a) {
-  constexpr uint32_t kLanes = D / 4;
-  const uint64_t all = (uint64_t)a.tokens * (a.p.kv_heads * a.rep);
-  const uint64_t pair = (uint64_t)blockIdx.x * (kJoinThreads / kLanes) + threadIdx.x / kLanes;
-  const uint32_t at = threadIdx.x % kLanes;
-  const uint32_t used = (uint32_t)a.starts[a.p.rows];                  // tokens behind the last sequence have no parts
-  if (pair >= all || pair / (a.p.kv_heads * a.rep) >= used || pair / (a.p.kv_heads * a.rep) < (uint32_t)a.starts[0]) return;
-  constexpr uint32_t kAtOnce = 8;
+  constexpr uint32_t kLanes = D / 4, kAtOnce = 8;
+  const uint32_t lane = threadIdx.x % kWaveSize, q_heads = a.p.kv_heads * a.rep, token = blockIdx.x;
+  const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)find_row(a.p.rows, lane, [&](uint32_t b) { return (uint32_t)a.starts[b] <= token; }));
+  const int32_t start = a.starts[row], end = a.starts[row + 1u];
+  if (start < 0 || (uint32_t)start > token || end <= (int32_t)token || (uint32_t)end > a.tokens) return;      // nobody's token has no parts
+  const uint32_t count = (uint32_t)(end - start), skip = (token - (uint32_t)start) / a.per * a.per;
+  const int32_t length = (int32_t)held(a.p.lens[row], a.p.row_pages, a.p.page_shift);
+  const KeyTiles key_tiles = key_tiles_of(length - (int32_t)count + (int32_t)skip, min(a.per, count - skip), (int32_t)a.window, (int32_t)min(a.sinks, 0x7FFFFFFFu), KEYS);
+  const uint32_t splits = prompt_splits(key_tiles.tiles * KEYS, a.splits);
+  if (splits == 1u) return;                                            // finished where it was
+  const uint32_t hq = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, at = threadIdx.x % kLanes;
+  if (hq >= q_heads) return;
+  const uint64_t all = (uint64_t)a.tokens * q_heads, pair = (uint64_t)token * q_heads + hq;
   float m = -INFINITY, l = 0.0f;
   f32x4 o = (f32x4)(0.0f);
-  for (uint32_t s = 0; s < a.splits; s += kAtOnce) {
+  for (uint32_t s = 0; s < splits; s += kAtOnce) {
     f32x2 ml[kAtOnce];
     f32x4 x[kAtOnce];
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
-      const uint64_t slot = min(s + k, a.splits - 1u) * all + pair;    // past the last one: the last one, without weight
+      const uint64_t slot = min(s + k, splits - 1u) * all + pair;      // past the last one: the last one, without weight
       ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
       x[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
     }
     float top = m;
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
-      if (s + k >= a.splits) ml[k].x = -INFINITY;
+      if (s + k >= splits) ml[k].x = -INFINITY;
       top = fmaxf(top, ml[k].x);
     }
     const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top);
@@ -478,26 +484,17 @@ void launch_prompt_run(const PagedPromptArgs& a, hipStream_t stream) {
   else prompt_kernel<T, D, 1u, SPLIT, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
 }
 
-template <typename T, int D, bool SPLIT>
-void launch_prompt_waves(const PagedPromptArgs& a, hipStream_t stream) {
-  if constexpr (D != 256) {
-    if (a.waves == 8u) return launch_prompt_run<T, D, SPLIT, 8u>(a, stream);
-  }
-  launch_prompt_run<T, D, SPLIT, 4u>(a, stream);
-}
-
 template <typename T, int D>
 hipError_t launch_prompt_of(const PagedPromptArgs& a, hipStream_t stream) {
   if (a.splits == 1u) {
-    launch_prompt_waves<T, D, false>(a, stream);
+    if (D == 128 && a.waves == 8u) launch_prompt_run<T, 128, false, 8u>(a, stream);
+    else launch_prompt_run<T, D, false, 4u>(a, stream);
     return hipGetLastError();
   }
-  launch_prompt_waves<T, D, true>(a, stream);
+  launch_prompt_run<T, D, true, 4u>(a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const uint64_t pairs = (uint64_t)a.tokens * (a.p.kv_heads * a.rep);
-  constexpr uint32_t kPairs = kJoinThreads / (D / 4);
-  prompt_join_kernel<T, D><<<(uint32_t)((pairs + kPairs - 1u) / kPairs), kJoinThreads, 0, stream>>>(a);
+  prompt_join_kernel<T, D, prompt_keys(4u)><<<dim3(a.tokens, (a.p.kv_heads * a.rep + kJoinThreads / (D / 4) - 1u) / (kJoinThreads / (D / 4))), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -89,8 +89,31 @@ static int query_places() {
   return 0;
 }
 
+static int keys_of_queries() {
+  for (int round = 0; round < 4000; ++round) {
+    const int32_t base = (int32_t)draw(500) - (round % 7 ? 0 : 40), window = draw(3) ? (int32_t)draw(300) + 1 : 0, sinks = window ? (int32_t)draw(round % 5 ? 70 : 600) : 0;
+    const uint32_t here = 1u + draw(130), keys = draw(2) ? 32u : 64u;
+    const int32_t reach = base + (int32_t)here;
+    const KeyTiles k = key_tiles_of(base, here, window, sinks, keys);
+    std::vector<int> count(reach > 0 ? reach : 0, 0);
+    for (uint32_t i = 0; i < k.tiles; ++i) {
+      const uint32_t t = (i < k.head ? i : k.body + (i - k.head)) * keys;
+      CHECK(reach > 0 && t < (uint32_t)reach);
+      for (uint32_t j = t; j < t + keys && j < (uint32_t)reach; ++j) ++count[j];
+    }
+    for (int32_t t = 0; t < reach; ++t) {
+      bool seen = false;
+      for (int32_t p = base; p < reach; ++p) seen = seen || (p >= 0 && t <= p && (window == 0 || t > p - window || t < sinks));
+      CHECK(count[t] <= 1 && (!seen || count[t] == 1));
+      CHECK(!seen || t >= k.win_lo || t < (int32_t)k.sink_end);
+    }
+    CHECK(prompt_splits(k.tiles * keys, 7u) >= 1u && prompt_splits(k.tiles * keys, 7u) <= (k.tiles > 1u ? k.tiles : 1u));
+  }
+  return 0;
+}
+
 int main() {
-  if (ranges() || deals() || query_places()) return 1;
+  if (ranges() || deals() || query_places() || keys_of_queries()) return 1;
   std::printf("ok\n");
   return 0;
 }
