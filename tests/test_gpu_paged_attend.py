@@ -5,7 +5,7 @@ import torch
 
 import paper_2605_03884_amd as qkv
 from oracle import paged_ref
-from paged_case import TYPES, Cache, check_attend
+from paged_case import TYPES, Cache, check_attend, check_prompt
 
 pytestmark = pytest.mark.gpu
 
@@ -75,6 +75,50 @@ def test_long_and_many_rows(lens, heads, q_heads):
     cache = Cache(lens, heads, 64, 16, seed=len(lens))
     q, out, lse = run(cache, q_heads, 64, 0.2)
     check_attend(out, lse, expected(cache, q, 0.2), 64, max(lens))
+
+
+@pytest.mark.parametrize("size", [8, 16, 64])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_page_sizes_of_other_dimensions(size, dim):
+    cache = Cache([300, 0, 64, 7], 1, dim, size, seed=size)
+    q, out, lse = run(cache, 3, dim, 0.07)
+    check_attend(out, lse, expected(cache, q, 0.07), dim, 300)
+
+
+def test_rows_beyond_one_wave_in_parts():
+    lens = [(i * 37) % 90 for i in range(200)]
+    lens[130] = 4000
+    cache = Cache(lens, 1, 64, 16, seed=31)
+    q, out, lse = run(cache, 2, 64, 0.2, window=3000, sinks=2)
+    check_attend(out, lse, expected(cache, q, 0.2, 3000, 2), 64, 4000)
+
+
+def test_pages_behind_four_gigabytes():
+    """Offsets of pages pass 32 bits; what lies between is not touched."""
+    pages, size, dim, n = 300000, 64, 128, 500
+    k, v = (torch.empty(pages, 1, size, dim, dtype=torch.float16, device="cuda") for _ in range(2))
+    numbers = [pages - 1, 7, pages - 2, 262144, 131072, pages // 2, 262143, 1]
+    gen = torch.Generator().manual_seed(1)
+    dense = [torch.randn(len(numbers), size, dim, generator=gen).half() for _ in range(2)]
+    for i, page in enumerate(numbers):
+        k[page, 0], v[page, 0] = dense[0][i].cuda(), dense[1][i].cuda()
+    table, lens = torch.tensor([numbers], dtype=torch.int32, device="cuda"), torch.tensor([n], dtype=torch.int32, device="cuda")
+    p = qkv.Pages.make([k], [v], table, lens)
+    q = torch.randn(1, 4, dim, generator=gen).half()
+    out, lse = torch.empty(1, 4, dim, device="cuda"), torch.empty(1, 4, device="cuda")
+    qkv.paged_attend(p, q.cuda(), 0.09, out, lse)
+    K, V = (x.reshape(1, -1, dim)[:, :n].double().numpy() for x in dense)
+    want = paged_ref.attend(q.double().numpy(), K, V, [n - 1], 0.09)
+    check_attend(out.double().cpu().numpy(), lse.double().cpu().numpy(), want, dim, n)
+    starts = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    new = torch.randn(3, 1, dim, generator=gen).half()
+    qkv.pages_append(p, new.cuda(), -new.cuda(), starts=starts)              # places 497 .. 499: page 1
+    assert torch.equal(k[1, 0, 49:52].cpu(), new[:, 0]) and torch.equal(v[1, 0, 49:52].cpu(), -new[:, 0])
+    half = torch.empty(3, 4, dim, dtype=torch.float16, device="cuda")
+    qkv.paged_prompt(p, q.cuda().expand(3, 4, dim).contiguous(), starts, 0.09, half)
+    K[:, 497:500], V[:, 497:500] = new.double().numpy().transpose(1, 0, 2), -new.double().numpy().transpose(1, 0, 2)
+    want = paged_ref.attend(q.double().numpy().repeat(3, 0), K, V, [497, 498, 499], 0.09)
+    check_prompt(half.double().cpu().numpy(), None, want, dim, n, "fp16", float(np.abs(V).max()))
 
 
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 1e-20, 40.0])

@@ -34,6 +34,28 @@ def expected(cache, new, q, scale, window=0, sinks=0, absent=None, layer=0):
     return [np.concatenate(x) for x in zip(*parts)]
 
 
+def expected_fast(cache, new, q, scale, window=0, sinks=0):
+    """expected() with whole matrices of a head at a time (torch, float64, on the CPU): the same definition for sizes that token by token take too long."""
+    parts, at = [], 0
+    for b, (K, V) in enumerate(cache.rows()):
+        n, (H, T, D) = new[b], K.shape
+        place, t = torch.arange(T - n, T)[:, None], torch.arange(T)[None]
+        seen = (t <= place) & ((t > place - window) | (t < sinks)) if window else t <= place
+        x, heads = q[at:at + n].double(), q.shape[1]
+        got = [torch.zeros(n, heads, D, dtype=torch.float64), torch.full((n, heads), -float("inf"), dtype=torch.float64), torch.zeros(n, heads, D, dtype=torch.float64),
+               torch.zeros(n, heads, dtype=torch.float64), torch.zeros(n, heads, dtype=torch.float64)]
+        for h in range(heads if n else 0):
+            k, v = (torch.from_numpy(np.ascontiguousarray(y[h // (heads // H)])) for y in (K, V))
+            s = (x[:, h] @ k.T) * scale
+            p = torch.softmax(s.masked_fill(~seen, -float("inf")), 1)
+            got[0][:, h], got[1][:, h], got[2][:, h] = p @ v, torch.logsumexp(s.masked_fill(~seen, -float("inf")), 1), p @ v.abs()
+            got[3][:, h] = (abs(scale) * (x[:, h].abs() @ k.abs().T)).masked_fill(~seen, 0).amax(1)
+            got[4][:, h] = s.abs().masked_fill(~seen, 0).amax(1)
+        parts.append([y.numpy() for y in got])
+        at += n
+    return [np.concatenate(y) for y in zip(*parts)]
+
+
 def check(cache, new, got, want, dim):
     q, out, lse = got
     most = max([float(np.abs(V).max()) for _, V in cache.rows() if V.size] + [1.0])
@@ -84,6 +106,59 @@ def test_few_queries_behind_many_keys(new, old, window):
     assert qkv.paged_prompt_workspace(cache.pages, 4, sum(new) + 3) > 0
     got = run(cache, new, 4, 64, 0.125, window=window, sinks=2 if window else 0)
     check(cache, new, got, expected(cache, new, got[0], 0.125, window, 2 if window else 0), 64)
+
+
+@pytest.mark.parametrize("kind,size,window,sinks", [("fp16", 64, 0, 0), ("bf16", 16, 0, 0), ("fp16", 8, 300, 5), ("bf16", 128, 70, 0)])
+def test_large_prompts(kind, size, window, sinks):
+    """As many (token, head) pairs as give every CU a tile of 256: another kernel than small prompts have."""
+    new, old = [1500, 0, 3, 640], [77, 10, 0, 1000]
+    cache = Cache([a + b for a, b in zip(new, old)], 4, 128, size, kind, seed=size)
+    got = run(cache, new, 32, 128, 0.09, window=window, sinks=sinks)
+    check(cache, new, got, expected_fast(cache, new, got[0], 0.09, window, sinks), 128)
+    assert int(cache.status) == 0
+
+
+def test_large_prompts_with_an_entry_that_names_no_page_and_infinite_values():
+    cache = Cache([2100], 1, 128, 16, seed=8)
+    lost = set(range(1600, 1616))
+    cache.v[0, cache.table[0, 125], 0, 3, 100] = float("inf")
+    cache.gpu()
+    cache.gtable[0, 100] = -1
+    q, out, lse = run(cache, [2100], 32, 128, 0.09)
+    assert int(cache.status) == qkv.STATUS_BAD_PAGE
+    assert np.isposinf(out[2003:, :, 100]).all() and np.isfinite(out[:2003]).all()
+    few = [0, 1, 1599, 1600, 1615, 1700, 2002, 2003, 2099]
+    K, V = cache.rows()[0]
+    V = np.where(np.isfinite(V), V, 0.0)
+    want = paged_ref.attend(q[few].double().numpy(), K, V, few, 0.09, absent=lost)
+    out = out[few]
+    out[7:, :, 100] = want[0][7:, :, 100]
+    check_prompt(out, lse[few], want, 128, 2100, "fp16", float(np.abs(V).max()))
+
+
+@pytest.mark.parametrize("size", [8, 32, 64])
+@pytest.mark.parametrize("dim", [64, 256])
+def test_page_sizes_of_other_dimensions(size, dim):
+    new, lens = [40, 100, 3], [40, 150, 64]
+    cache = Cache(lens, 1, dim, size, seed=size)
+    got = run(cache, new, 3, dim, 0.07)
+    check(cache, new, got, expected(cache, new, got[0], 0.07), dim)
+
+
+def test_short_and_long_sequences_in_a_wide_table():
+    """The host allows parts; only the long sequences have them."""
+    new, old = [9, 1, 30, 0, 4], [0, 1100, 3, 6000, 600]
+    cache = Cache([a + b for a, b in zip(new, old)], 2, 64, 16, seed=21, extra_entries=3000)
+    assert qkv.paged_prompt_workspace(cache.pages, 4, sum(new) + 3) > 0
+    got = run(cache, new, 4, 64, 0.125)
+    check(cache, new, got, expected(cache, new, got[0], 0.125), 64)
+
+
+def test_many_rows():
+    new = [(i * 7) % 5 for i in range(300)]
+    cache = Cache([n + i % 9 for i, n in enumerate(new)], 1, 64, 8, seed=22)
+    got = run(cache, new, 2, 64, 0.125)
+    check(cache, new, got, expected(cache, new, got[0], 0.125), 64)
 
 
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 3.0])
