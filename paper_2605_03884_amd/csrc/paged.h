@@ -17,7 +17,8 @@
 namespace qkv {
 
 constexpr uint32_t kAttendTile = 32;         // tokens a wave of the decode kernel takes at a time
-constexpr uint32_t kAttendLeast = 4;         // tiles a share has at least, where the work is split at all
+constexpr uint32_t kAttendWhole = 4;         // tiles of the longest sequence there is room for, up to which items are not cut at all
+constexpr uint32_t kAttendLeast = 2;         // tiles a share has at least, where items are cut
 constexpr uint32_t kMaxRows = 65536;         // sequences of a table
 
 // The tokens a query at the last position of `length` sees: [0, sink_end) and [begin, length).
@@ -72,6 +73,8 @@ QKV_HD Shares deal(uint32_t total, uint32_t most) {
   if (total <= kAttendLeast * most) return Shares{(total + kAttendLeast - 1u) / kAttendLeast, kAttendLeast, 0u, total};
   return Shares{most, total / most, total % most, total};
 }
+// Items that are not cut: share i has the items [i * each, (i + 1) * each).
+QKV_HD uint32_t items_each(uint32_t items, uint32_t most) { return (items + most - 1u) / most; }
 QKV_HD uint32_t share_begin(const Shares& s, uint32_t i) {
   const uint32_t at = i * s.each + (i < s.more ? i : s.more);
   return at < s.total ? at : s.total;
@@ -159,6 +162,7 @@ struct PagedAttendArgs {
   float *out, *lse;
   float *part_o, *part_ml;                               // [items + most shares][heads of a block][dim], [...][2]
   uint32_t most;                                         // shares at most
+  uint32_t cut;                                          // items may be cut: tiles are dealt, otherwise items
   uint32_t* status;
 };
 

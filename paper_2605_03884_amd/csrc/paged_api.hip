@@ -115,7 +115,7 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
   a.heads = a.rep < 16u ? a.rep : 16u;
   a.items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
   if (a.items * most_tiles(p) >= (1ull << 31) || a.items >= (1ull << 22)) return QKV_ERR_SHAPE;
-  a.split = most_tiles(p) - 2u > kAttendLeast;
+  a.split = most_tiles(p) - 2u > kAttendWhole;
   // Waves: as many as the chip holds at once at the kernel's registers (64 dimensions: three quarters, 3072 took 32.6 us where 2048 take 32.0),
   // or as many as have 4 tiles each.
   const uint64_t shares = (a.items * most_tiles(p) + kAttendLeast - 1u) / kAttendLeast, fit = p->head_dim == 256 ? 1024u : 2048u;
@@ -272,6 +272,7 @@ int qkv_paged_attend(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   a.part_o = static_cast<float*>(query->workspace_dev);
   a.part_ml = plan.floats ? a.part_o + (plan.items + plan.most) * plan.heads * (uint64_t)pages->head_dim : nullptr;
   a.most = plan.most;
+  a.cut = plan.split ? 1u : 0u;
   a.status = query->status_dev;
   return launch_paged_attend(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, plan.split, static_cast<hipStream_t>(stream)) ==
                  hipSuccess ? QKV_OK : QKV_ERR_HIP;

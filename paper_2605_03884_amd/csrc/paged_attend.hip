@@ -143,27 +143,38 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
   const uint32_t n = lane % 16u, g = lane / 16u;
   const uint32_t inner_count = a.p.kv_heads * a.blocks, q_heads = a.p.kv_heads * a.rep;
-  const Lengths lengths = read_lengths(a, lane);
-  const Shares shares = deal(lengths.total * inner_count, a.most);
   const uint32_t share = blockIdx.x * kAttendWaves + wave;
-  if (share >= shares.shares) return;
-  uint32_t at = share_begin(shares, share);
-  const uint32_t end = share_begin(shares, share + 1u);
-  uint32_t before, length;
-  uint32_t row = row_of_tile(a, lengths, lane, inner_count, at, before, length);
+  uint32_t row, inner, tile = 0u, length, at = 0u, end = 0xFFFFFFFFu, left = 0xFFFFFFFFu;       // left: items, where they are not cut
+  if (a.cut) {
+    const Lengths lengths = read_lengths(a, lane);
+    const Shares shares = deal(lengths.total * inner_count, a.most);
+    if (share >= shares.shares) return;
+    at = share_begin(shares, share);
+    end = share_begin(shares, share + 1u);
+    uint32_t before;
+    row = row_of_tile(a, lengths, lane, inner_count, at, before, length);
+    const uint32_t tiles = seen_tiles(seen_by_last(length, a.window, a.sinks));
+    // the item of the row, by counting those that end in front of `at`: a division took longer
+    inner = 0u;
+    for (uint32_t base = 0; base < inner_count; base += kWaveSize) {
+      const uint64_t ended = __builtin_amdgcn_ballot_w64(base + lane < inner_count && before + (base + lane + 1u) * tiles <= at);
+      inner += (uint32_t)__builtin_popcountll(ended);
+      if (ended != ~0ull) break;
+    }
+    tile = at - before - inner * tiles;
+  } else {
+    const uint32_t items = a.p.rows * inner_count, each = items_each(items, a.most), item = share * each;
+    if (item >= items) return;
+    left = min(each, items - item);
+    row = item / inner_count;
+    inner = item % inner_count;
+    length = row_length(a, row);
+  }
   Seen seen = seen_by_last(length, a.window, a.sinks);
   uint32_t tiles = seen_tiles(seen);
-  // the item of the row, by counting those that end in front of `at`: a division took longer
-  uint32_t inner = 0u;
-  for (uint32_t base = 0; base < inner_count; base += kWaveSize) {
-    const uint64_t ended = __builtin_amdgcn_ballot_w64(base + lane < inner_count && before + (base + lane + 1u) * tiles <= at);
-    inner += (uint32_t)__builtin_popcountll(ended);
-    if (ended != ~0ull) break;
-  }
-  uint32_t tile = at - before - inner * tiles;
   uint8_t* mine = lds[wave];
 
-  while (at < end) {
+  for (;;) {
     // one item, or what of it falls into this share
     const uint32_t head = a.blocks == 1u ? inner : inner / a.blocks, block = a.blocks == 1u ? 0u : inner % a.blocks;
     const uint32_t heads = min(16u, a.rep - block * 16u);
@@ -299,7 +310,8 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
 
     at += upto - from;
     tile = 0u;
-    if (++inner == inner_count && at < end) {
+    if (--left == 0u || at >= end) return;
+    if (++inner == inner_count) {
       inner = 0u;
       ++row;
       seen = seen_by_last((uint32_t)__builtin_amdgcn_readfirstlane((int)row_length(a, row)), a.window, a.sinks);

@@ -65,6 +65,8 @@ static int deals() {
       }
     }
     CHECK(item == items);
+    const uint32_t each = items_each(items, most);          // items that are not cut: every one in one of `most` shares
+    CHECK(each >= 1u && (uint64_t)each * most >= items && each * ((items + each - 1u) / each) >= items && (items + each - 1u) / each <= most);
   }
   return 0;
 }

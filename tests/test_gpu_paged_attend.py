@@ -77,6 +77,25 @@ def test_long_and_many_rows(lens, heads, q_heads):
     check_attend(out, lse, expected(cache, q, 0.2), 64, max(lens))
 
 
+@pytest.mark.parametrize("lens", [[90, 65, 70], [128, 0, 97, 33, 1], [66] * 40])
+@pytest.mark.parametrize("heads,q_heads", [(1, 1), (3, 6)])
+def test_room_for_few_tokens(lens, heads, q_heads):
+    """A table with room for 128 tokens a row: no sequence is cut, and no workspace is needed."""
+    cache = Cache(lens, heads, 64, 16, seed=len(lens), extra_entries=8 - max(-(-n // 16) for n in lens))
+    assert qkv.paged_attend_workspace(cache.pages, q_heads) == 0
+    q, out, lse = run(cache, q_heads, 64, 0.125)
+    check_attend(out, lse, expected(cache, q, 0.125), 64, 128)
+    windowed = run(cache, q_heads, 64, 0.125, window=40, sinks=3)
+    check_attend(windowed[1], windowed[2], expected(cache, q, 0.125, 40, 3), 64, 128)
+
+
+def test_more_items_than_shares_that_are_not_cut():
+    cache = Cache([(i * 13) % 60 for i in range(700)], 4, 64, 16, seed=5, extra_entries=0)
+    assert qkv.paged_attend_workspace(cache.pages, 4) == 0
+    q, out, lse = run(cache, 4, 64, 0.125)
+    check_attend(out, lse, expected(cache, q, 0.125), 64, 60)
+
+
 @pytest.mark.parametrize("size", [8, 16, 64])
 @pytest.mark.parametrize("dim", [64, 256])
 def test_page_sizes_of_other_dimensions(size, dim):
