@@ -69,8 +69,21 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   // the tile: sequence, queries, keys
   const uint32_t kv_head = blockIdx.x % a.p.kv_heads;
   const uint32_t at = gridDim.x / a.p.kv_heads - 1u - blockIdx.x / a.p.kv_heads;      // tiles with many keys first
-  const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)find_row(a.p.rows, lane, [&](uint32_t b) { return first_place((uint32_t)a.starts[b], b, a.per) <= at; }));
-  const int32_t start = a.starts[row], end = a.starts[row + 1u];
+  uint32_t row;
+  int32_t start, end, raw_length;
+  if (a.p.rows < kWaveSize) {                                          // one trip to memory: lane l has row l's start and length
+    const int32_t mine = a.starts[min(lane, a.p.rows)], long_is = a.p.lens[min(lane, a.p.rows - 1u)];
+    const uint64_t fits = __builtin_amdgcn_ballot_w64(lane < a.p.rows && first_place((uint32_t)mine, lane, a.per) <= at);
+    row = fits ? 63u - (uint32_t)__builtin_clzll(fits) : 0u;
+    start = __builtin_amdgcn_readlane(mine, (int)row);
+    end = __builtin_amdgcn_readlane(mine, (int)row + 1);
+    raw_length = __builtin_amdgcn_readlane(long_is, (int)row);
+  } else {
+    row = (uint32_t)__builtin_amdgcn_readfirstlane((int)find_row(a.p.rows, lane, [&](uint32_t b) { return first_place((uint32_t)a.starts[b], b, a.per) <= at; }));
+    start = a.starts[row];
+    end = a.starts[row + 1u];
+    raw_length = a.p.lens[row];
+  }
   if (start < 0 || end < start || (uint32_t)end > a.tokens) {
     if (threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_ROW);
     return;
@@ -78,7 +91,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   const uint32_t count = (uint32_t)(end - start), skip = (at - first_place((uint32_t)start, row, a.per)) * a.per;
   if (at < first_place((uint32_t)start, row, a.per) || skip >= count) return;
   const uint32_t here = min(a.per, count - skip);                      // query tokens
-  const int32_t length = (int32_t)held(a.p.lens[row], a.p.row_pages, a.p.page_shift);
+  const int32_t length = (int32_t)held(raw_length, a.p.row_pages, a.p.page_shift);
   const int32_t base = length - (int32_t)count + (int32_t)skip;        // place of the tile's first query
   if (base < 0 && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_ROW);
   const int32_t window = (int32_t)a.window, sinks = (int32_t)min(a.sinks, 0x7FFFFFFFu);
