@@ -51,7 +51,7 @@ __device__ inline bool take_out(u32x4& x) {
   return any;
 }
 
-template <typename T, int D, uint32_t RUN, bool SPLIT, uint32_t WAVES>
+template <typename T, int D, uint32_t RUN, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void prompt_kernel(PagedPromptArgs a) {
   constexpr uint32_t kThreads = WAVES * kWaveSize;
   constexpr uint32_t kKeys = prompt_keys(WAVES), kHalves = kKeys / 32u;    // keys of a tile; scores are worked out 32 keys at a time
@@ -99,10 +99,9 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   const KeyTiles key_tiles = key_tiles_of(base, here, window, sinks, kKeys);
   const int32_t win_lo = key_tiles.win_lo;
   const uint32_t sink_end = key_tiles.sink_end, head = key_tiles.head, body = key_tiles.body, tiles = key_tiles.tiles;
-  const uint32_t splits = SPLIT ? prompt_splits(tiles * kKeys, a.splits) : 1u;
-  if (SPLIT && blockIdx.y >= splits) return;
-  const uint32_t first_tile = SPLIT ? (uint32_t)((uint64_t)tiles * blockIdx.y / splits) : 0u;
-  const uint32_t last_tile = SPLIT ? (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / splits) : tiles;
+  const uint32_t splits = prompt_splits(tiles * kKeys, a.splits);
+  if (blockIdx.y >= splits) return;
+  const uint32_t first_tile = (uint32_t)((uint64_t)tiles * blockIdx.y / splits), last_tile = (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / splits);
   const auto tile_at = [&](uint32_t i) -> int32_t { return (int32_t)((i < head ? i : body + (i - head)) * kKeys); };
   // Tiles [from, from + count) are seen whole by all queries at places [lo, hi]; those of the sinks are not counted among them.
   struct Range {
@@ -411,7 +410,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     }
     const uint64_t out_at = query * q_heads + hq;
     const float sum = sum32(l);
-    if (SPLIT && splits != 1u) {
+    if (splits != 1u) {
       const uint64_t slot = (uint64_t)blockIdx.y * a.tokens * q_heads + out_at;
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d)
@@ -489,24 +488,20 @@ __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptAr
   if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-template <typename T, int D, bool SPLIT, uint32_t WAVES>
+template <typename T, int D, uint32_t WAVES>
 void launch_prompt_run(const PagedPromptArgs& a, hipStream_t stream) {
   const dim3 grid(places(a.tokens, a.p.rows, a.per) * a.p.kv_heads, a.splits);
-  if (a.p.page_shift >= 6u) prompt_kernel<T, D, 64u, SPLIT, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
-  else if (a.p.page_shift >= 4u) prompt_kernel<T, D, 16u, SPLIT, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
-  else prompt_kernel<T, D, 1u, SPLIT, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
+  if (a.p.page_shift >= 6u) prompt_kernel<T, D, 64u, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
+  else if (a.p.page_shift >= 4u) prompt_kernel<T, D, 16u, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
+  else prompt_kernel<T, D, 1u, WAVES><<<grid, WAVES * kWaveSize, 0, stream>>>(a);
 }
 
 template <typename T, int D>
 hipError_t launch_prompt_of(const PagedPromptArgs& a, hipStream_t stream) {
-  if (a.splits == 1u) {
-    if (D == 128 && a.waves == 8u) launch_prompt_run<T, 128, false, 8u>(a, stream);
-    else launch_prompt_run<T, D, false, 4u>(a, stream);
-    return hipGetLastError();
-  }
-  launch_prompt_run<T, D, true, 4u>(a, stream);
+  if (D == 128 && a.waves == 8u) launch_prompt_run<T, 128, 8u>(a, stream);
+  else launch_prompt_run<T, D, 4u>(a, stream);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.splits == 1u) return e;
   prompt_join_kernel<T, D, prompt_keys(4u)><<<dim3(a.tokens, (a.p.kv_heads * a.rep + kJoinThreads / (D / 4) - 1u) / (kJoinThreads / (D / 4))), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
