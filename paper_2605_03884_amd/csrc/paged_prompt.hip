@@ -155,7 +155,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   };
   const uint32_t own = my_row % RUN * (RUN == 1u ? 0u : (uint32_t)a.p.token_stride) + my_chunk * 16u;
   uint64_t lost = 0ull;
-  bool any_lost = false;
+  uint32_t any_lost = 0u;                                              // the same for all waves: they look at the same entries
   const auto settle = [&](uint32_t i, uint32_t entry) -> Spots {
     const int32_t t = tile_at(i);
     uint32_t page = entry;
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
       const bool wanted = lane < kKeys && seen_by_some(t + (int32_t)lane), known = entry < a.p.pages;
       there = __builtin_amdgcn_ballot_w64(wanted && known);
       lost = __builtin_amdgcn_ballot_w64(wanted && !known);
-      any_lost = any_lost || lost != 0ull;
+      any_lost = (uint32_t)__builtin_amdgcn_readfirstlane((int)(any_lost | (lost != 0ull ? 1u : 0u)));
       page = wanted && known ? entry : 0u;
     }
     Spots to;
@@ -196,18 +196,18 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(k_rows + at + j * kRowsAtOnce * key_row(D)) = x[j];
   };
   const auto store_values = [&](uint32_t i, uint32_t at) {
-    if (!holds(whole_to_all, i) || any_lost) {                         // only there can a value meet a weight that has to be nothing
-      if (any_lost) {
+    if (!holds(whole_to_all, i) || any_lost != 0u) {                         // only there can a value meet a weight that has to be nothing
+      if (any_lost != 0u) {
         lost = 0ull;
         settle(i, look_up(i));
       }
 #pragma unroll
       for (uint32_t j = 0; j < kLoads; ++j) {
         const uint32_t of = j * kRowsAtOnce + my_row;
-        if (!seen_by_some(tile_at(i) + (int32_t)of) || (any_lost && (lost >> of & 1ull))) vx[j] = (u32x4)(0u);
+        if (!seen_by_some(tile_at(i) + (int32_t)of) || (any_lost != 0u && (lost >> of & 1ull))) vx[j] = (u32x4)(0u);
         if (take_out<T>(vx[j])) taken_out = 1u;
       }
-      if (any_lost && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
+      if (any_lost != 0u && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
     }
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(v_rows + at + j * kRowsAtOnce * value_row(D)) = vx[j];
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     const auto below = [](int32_t n) { return (uint32_t)((1ull << (uint32_t)min(max(n, 0), 32)) - 1ull); };
     uint32_t seen = below(mine - t + 1);
     if (window != 0) seen &= ~below(mine - t - window + 1) | below(sinks - t);
-    if (any_lost) {
+    if (any_lost != 0u) {
       lost = 0ull;
       settle(i, look_up(i));
       seen &= ~(uint32_t)(lost >> (32u * half));
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
 #pragma unroll
     for (uint32_t j = 0; j < 16u; ++j) s[j] = seen >> (8u * (j / 4u) + j % 4u) & 1u ? s[j] : -INFINITY;
   };
-  const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || any_lost; };
+  const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || any_lost != 0u; };
   // m, which is -inf at first, to the largest score there is
   const auto follow = [&]() {
     const float most = max32(top) * a.scale_log2;
