@@ -242,10 +242,12 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
 #pragma unroll
         for (uint32_t j = 0; j < kLoads; ++j) vx[j] = (counted >> (j * kRowsAtOnce + lane / kRowLanes)) & 1u ? vx[j] : (u32x4)(0u);
       }
-      float e[8];
-      float top = s[0][0] * a.scale_log2;
+      float e[8];                                                      // the scores, then their weights
 #pragma unroll
-      for (uint32_t j = 1; j < 8u; ++j) top = fmaxf(top, s[j / 4u][j % 4u] * a.scale_log2);
+      for (uint32_t j = 0; j < 8u; ++j) e[j] = s[j / 4u][j % 4u] * a.scale_log2;
+      float top = e[0];
+#pragma unroll
+      for (uint32_t j = 1; j < 8u; ++j) top = fmaxf(top, e[j]);
       top = max32(max16(top));
       const float m_new = fmaxf(m, top);
       const float less = m_new == -INFINITY ? 0.0f : m_new - kLift;    // what is taken off in the exponent
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
         m = m_new;
       }
 #pragma unroll
-      for (uint32_t j = 0; j < 8u; ++j) e[j] = exp2f_(__builtin_fmaf(s[j / 4u][j % 4u], a.scale_log2, -less));
+      for (uint32_t j = 0; j < 8u; ++j) e[j] = exp2f_(e[j] - less);    // rounded as the maximum is: none is above 2^16, however large the scores
       l += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       typename T::x8 w[T::kParts];
       T::parts(e, w);

@@ -23,6 +23,10 @@ namespace qkv {
 namespace {
 
 constexpr float kLift = 7.0f, kSlack = 8.0f;
+// From here on a maximum's rounding counts in an exponent that is not rounded: scores are multiplied with the scale by themselves, and m follows at once.
+constexpr float kFar = 0x1p20f;
+constexpr uint32_t kLost = 1u, kScaled = 2u;             // what a wave has met: an entry that names no page, a maximum beyond kFar
+__device__ inline float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 
 // Rows of K and V in LDS are longer than they need to be, by 16 and 64 bytes: 16 lanes that read a piece of 16 bytes of as many rows of K, and 32 that
 // read 64 bytes of four rows of V through the transposing read, then meet every bank once.
@@ -134,6 +138,8 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
 #pragma unroll
   for (uint32_t d = 0; d < kSlabs; ++d) acc[d] = (f32x16)(0.0f);
   float m = -INFINITY, l = 0.0f, less = 0.0f;                          // less: what is taken off in the exponent
+  float scale = a.scale_log2, slack = kSlack;                          // 1 and 0 once a maximum was beyond kFar
+  uint32_t special = 0u;                                               // bits, the same for all lanes: kLost, kScaled
 
   const uint8_t* keys = a.p.k + (uint64_t)kv_head * a.p.head_stride;
   const uint8_t* values = a.p.v + (uint64_t)kv_head * a.p.head_stride;
@@ -155,7 +161,6 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   };
   const uint32_t own = my_row % RUN * (RUN == 1u ? 0u : (uint32_t)a.p.token_stride) + my_chunk * 16u;
   uint64_t lost = 0ull;
-  uint32_t any_lost = 0u;                                              // the same for all waves: they look at the same entries
   const auto settle = [&](uint32_t i, uint32_t entry) -> Spots {
     const int32_t t = tile_at(i);
     uint32_t page = entry;
@@ -164,7 +169,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
       const bool wanted = lane < kKeys && seen_by_some(t + (int32_t)lane), known = entry < a.p.pages;
       there = __builtin_amdgcn_ballot_w64(wanted && known);
       lost = __builtin_amdgcn_ballot_w64(wanted && !known);
-      any_lost = (uint32_t)__builtin_amdgcn_readfirstlane((int)(any_lost | (lost != 0ull ? 1u : 0u)));
+      special = (uint32_t)__builtin_amdgcn_readfirstlane((int)(special | (lost != 0ull ? kLost : 0u)));
       page = wanted && known ? entry : 0u;
     }
     Spots to;
@@ -196,18 +201,19 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(k_rows + at + j * kRowsAtOnce * key_row(D)) = x[j];
   };
   const auto store_values = [&](uint32_t i, uint32_t at) {
-    if (!holds(whole_to_all, i) || any_lost != 0u) {                         // only there can a value meet a weight that has to be nothing
-      if (any_lost != 0u) {
+    const bool any_lost = (special & kLost) != 0u;                     // in all waves or in none: they look at the same entries
+    if (!holds(whole_to_all, i) || any_lost) {                         // only there can a value meet a weight that has to be nothing
+      if (any_lost) {
         lost = 0ull;
         settle(i, look_up(i));
       }
 #pragma unroll
       for (uint32_t j = 0; j < kLoads; ++j) {
         const uint32_t of = j * kRowsAtOnce + my_row;
-        if (!seen_by_some(tile_at(i) + (int32_t)of) || (any_lost != 0u && (lost >> of & 1ull))) vx[j] = (u32x4)(0u);
+        if (!seen_by_some(tile_at(i) + (int32_t)of) || (any_lost && (lost >> of & 1ull))) vx[j] = (u32x4)(0u);
         if (take_out<T>(vx[j])) taken_out = 1u;
       }
-      if (any_lost != 0u && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
+      if (any_lost && threadIdx.x == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
     }
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) *reinterpret_cast<u32x4*>(v_rows + at + j * kRowsAtOnce * value_row(D)) = vx[j];
@@ -234,7 +240,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   const auto weigh = [&](const f32x16& s, uint32_t first, uint32_t count) {
     float e[16], sum = 0.0f;
 #pragma unroll
-    for (uint32_t j = first; j < first + count; ++j) e[j] = exp2f_(__builtin_fmaf(s[j], a.scale_log2, -less));
+    for (uint32_t j = first; j < first + count; ++j) e[j] = exp2f_(__builtin_fmaf(s[j], scale, -less));
 #pragma unroll
     for (uint32_t j = first; j < first + count; ++j) {
       asm volatile("" : "+v"(e[j]));                                   // here, and not behind the next branch
@@ -278,20 +284,29 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     const auto below = [](int32_t n) { return (uint32_t)((1ull << (uint32_t)min(max(n, 0), 32)) - 1ull); };
     uint32_t seen = below(mine - t + 1);
     if (window != 0) seen &= ~below(mine - t - window + 1) | below(sinks - t);
-    if (any_lost != 0u) {
-      lost = 0ull;
-      settle(i, look_up(i));
-      seen &= ~(uint32_t)(lost >> (32u * half));
+    if (special != 0u) {
+      if ((special & kLost) != 0u) {
+        lost = 0ull;
+        settle(i, look_up(i));
+        seen &= ~(uint32_t)(lost >> (32u * half));
+      }
+      if ((special & kScaled) != 0u) s *= a.scale_log2;
     }
     seen >>= 4u * h;
 #pragma unroll
     for (uint32_t j = 0; j < 16u; ++j) s[j] = seen >> (8u * (j / 4u) + j % 4u) & 1u ? s[j] : -INFINITY;
   };
-  const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || any_lost != 0u; };
-  // m, which is -inf at first, to the largest score there is
-  const auto follow = [&]() {
-    const float most = max32(top) * a.scale_log2;
-    if (__builtin_amdgcn_ballot_w64(most > m + kSlack) != 0ull) {
+  const auto masked = [&](uint32_t i) { return !holds(whole_to_wave, i) || special != 0u; };
+  // m, which is -inf at first, to the largest of the scores s
+  const auto follow = [&](f32x16& s) {
+    const float most = max32(top) * scale;
+    if (__builtin_amdgcn_ballot_w64(most > m + slack) != 0ull) {
+      if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(most) > kFar) != 0ull && (special & kScaled) == 0u) {
+        s *= scale;
+        scale = uniform(1.0f);
+        slack = uniform(0.0f);
+        special = (uint32_t)__builtin_amdgcn_readfirstlane((int)(special | kScaled));
+      }
       const float next = fmaxf(m, most);
       const float shrink = m == -INFINITY ? 0.0f : exp2f_(m - next);
       l *= shrink;
@@ -333,7 +348,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
     }
     if (masked(i)) mask(i, 0u, s_one);
     largest(s_one, 0u, 16u);
-    follow();
+    follow(s_one);
     if constexpr (kHalves == 2u) read_ahead(k_place[0] + 32u * key_row(D));
     __syncthreads();
     // 32 keys: the weights of `now` and their product with the values, beside the scores of the next 32 and their largest.
@@ -341,7 +356,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
       scores(k_at, v_at, next, now);
       if (masked(next_tile)) mask(next_tile, next_half, next);
       product(v_at, k_next, next);
-      follow();
+      follow(next);
     };
     const auto last_half = [&](const uint8_t* v_at, const f32x16& now) {
       weigh(now, 0u, 16u);
@@ -351,7 +366,8 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
         acc[k % kSlabs] = T::mfma32(v_piece[k], w[k / kSlabs], acc[k % kSlabs]);
       }
     };
-    for (; i + 1u < last_tile; ++i) {
+    // tile i, whose first scores are `now`; afterwards `next` has the next tile's, or where a tile is two halves `now` again
+    const auto step = [&](f32x16& now, f32x16& next) {
       // the keys of tile i + 2 and the values of i + 1 take places that nobody reads any more; those of i + 3 and i + 2 are asked for
       store_keys(kHalves == 2u ? k_free : k_now, kx);
       store_values(i + 1u, kValuePlace - v_now);
@@ -361,28 +377,36 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
       entry = look_up(no_further(i + 4u));
       const uint8_t *const v_at = v_place[0] + v_now, *const k_at = k_place[0] + k_now, *const k_then = k_place[0] + k_next;
       if constexpr (kHalves == 2u) {
-        half(k_at + 32u * key_row(D), v_at, k_then, s_one, s_two, i, 1u);
-        half(k_then, v_at + 32u * value_row(D), k_then + 32u * key_row(D), s_two, s_one, i + 1u, 0u);
+        half(k_at + 32u * key_row(D), v_at, k_then, now, next, i, 1u);
+        half(k_then, v_at + 32u * value_row(D), k_then + 32u * key_row(D), next, now, i + 1u, 0u);
         const uint32_t old = k_now;
         k_now = k_next;
         k_next = k_free;
         k_free = old;
       } else {
         read_ahead(k_then);                                            // the tile after it takes its place meanwhile, behind the barrier
-        half(k_then, v_at, k_then, s_one, s_two, i + 1u, 0u);
-        s_one = s_two;
+        half(k_then, v_at, k_then, now, next, i + 1u, 0u);
         k_now = k_next;
         k_next = kKeyPlace - k_next;
       }
       v_now = kValuePlace - v_now;
+      ++i;
       __syncthreads();
-    }
-    const uint8_t *const v_at = v_place[0] + v_now, *const k_at = k_place[0] + k_now;
+    };
     if constexpr (kHalves == 2u) {
-      half(k_at + 32u * key_row(D), v_at, k_at, s_one, s_two, i, 1u);
-      last_half(v_at + 32u * value_row(D), s_two);
+      while (i + 1u < last_tile) step(s_one, s_two);
+      half(k_place[0] + k_now + 32u * key_row(D), v_place[0] + v_now, k_place[0] + k_now, s_one, s_two, i, 1u);
+      last_half(v_place[0] + v_now + 32u * value_row(D), s_two);
     } else {
-      last_half(v_at, s_one);
+      while (i + 2u < last_tile) {
+        step(s_one, s_two);
+        step(s_two, s_one);
+      }
+      if (i + 1u < last_tile) {
+        step(s_one, s_two);
+        s_one = s_two;
+      }
+      last_half(v_place[0] + v_now, s_one);
     }
   }
 
@@ -419,14 +443,14 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
           *reinterpret_cast<f32x4*>(a.part_o + slot * D + d * 32u + j * 8u + h * 4u) = (f32x4){acc[d][4 * j], acc[d][4 * j + 1], acc[d][4 * j + 2], acc[d][4 * j + 3]};
       if (h == 0u) *reinterpret_cast<f32x2*>(a.part_ml + slot * 2u) = (f32x2){m, sum};
     } else {
-      const float scale = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
+      const float share = sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
         for (uint32_t j = 0; j < 4u; ++j) {
           typename T::x4 o;
 #pragma unroll
-          for (uint32_t e = 0; e < 4u; ++e) o[e] = (typename T::one)(acc[d][4u * j + e] * scale);
+          for (uint32_t e = 0; e < 4u; ++e) o[e] = (typename T::one)(acc[d][4u * j + e] * share);
           *reinterpret_cast<typename T::x4*>(a.out + (out_at * D + d * 32u + j * 8u + h * 4u) * 2u) = o;
         }
       if (a.lse && h == 0u) a.lse[out_at] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;

@@ -147,6 +147,15 @@ def test_scales(scale):
     check_attend(out, lse, expected(cache, q, float(np.float32(scale))), 64, 200)
 
 
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [3e5, -3e6, 1e8, 1e10])
+def test_scores_whose_steps_are_large(kind, scale):
+    """fp32 scores of 2^24 and more lie 2 and more apart, and so does a maximum that is rounded: a weight beside it may not overflow."""
+    cache = Cache([1, 90, 700, 2000], 2, 128, 16, kind)
+    q, out, lse = run(cache, 8, 128, scale)
+    check_attend(out, lse, expected(cache, q, scale), 128, 2000)
+
+
 def test_without_lse_and_with_a_larger_workspace():
     cache = Cache(LENGTHS, 2, 128, 16, seed=9)
     q, a, lse = run(cache, 8, 128, 0.1)

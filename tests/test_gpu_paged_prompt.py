@@ -168,6 +168,16 @@ def test_scales(scale):
     check(cache, [90, 10], got, expected(cache, [90, 10], got[0], float(np.float32(scale))), 64)
 
 
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [3e5, -3e6, 1e8, 1e10])
+def test_scores_whose_steps_are_large(kind, scale):
+    """fp32 scores of 2^24 and more lie 2 and more apart, and so does a maximum that is rounded: a weight beside it may not overflow."""
+    new, old = [60, 3, 90], [500, 1, 0]
+    cache = Cache([a + b for a, b in zip(new, old)], 2, 128, 16, kind)
+    got = run(cache, new, 8, 128, scale)
+    check(cache, new, got, expected(cache, new, got[0], scale), 128)
+
+
 def test_scores_that_rise_from_key_to_key():
     """The running maximum moves in every tile, by more and by less than what is put up with."""
     cache = Cache([300], 1, 64, 16, seed=5, strong=1.0)
