@@ -7,7 +7,6 @@ using namespace qkv;
 
 namespace {
 
-
 bool misaligned(const void* p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
 int check_pages(const qkv_pages_t* p, bool counted) {
@@ -116,9 +115,10 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
   a.items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
   if (a.items * most_tiles(p) >= (1ull << 31) || a.items >= (1ull << 22)) return QKV_ERR_SHAPE;
   a.split = most_tiles(p) - 2u > kAttendWhole;
-  // Waves: as many as the chip holds at once at the kernel's registers (64 dimensions: three quarters, 3072 took 32.6 us where 2048 take 32.0),
-  // or as many as have 4 tiles each.
-  const uint64_t shares = (a.items * most_tiles(p) + kAttendLeast - 1u) / kAttendLeast, fit = p->head_dim == 256 ? 1024u : 2048u;
+  // Waves: as many as the chip holds at once at 128 dimensions' registers, two a SIMD, or at 256 one, or as many as there may be tiles.  128 dimensions with one a
+  // SIMD: 48 rows of up to 8K tokens 150.5 us (with two 152), 200 of them 550 (545), 131071 tokens of one row 93 (96); 64 dimensions, 48 rows 97.5 (80.4); with
+  // three a SIMD 64 rows of 1004 seen tokens 32.8 (31.8).
+  const uint64_t shares = a.items * most_tiles(p), fit = p->head_dim == 256 ? 1024u : 2048u;
   a.most = (uint32_t)(shares < fit ? shares : fit);
   a.floats = a.split ? (a.items + a.most) * a.heads * ((uint64_t)p->head_dim + 2u) : 0u;
   return QKV_OK;

@@ -74,7 +74,7 @@ __device__ inline uint32_t row_of_tile(const PagedAttendArgs& a, const Lengths& 
   }
 }
 
-// RUN: tokens of a tile that surely lie in one page, one after the other: 32 or 16, or 1 where pages are smaller.
+// RUN: tokens of a tile that surely lie in one page, one after the other: 32, or 1 where pages are smaller.
 // The entry that lane l needs of a tile's pages: that of token l % 32, or where a page holds whole tiles the tile's.
 template <uint32_t RUN>
 __device__ inline uint32_t look_up(const PagedAttendArgs& a, uint32_t row, const TileRange& t, uint32_t lane) {
@@ -99,36 +99,20 @@ __device__ inline Tile settle(const PagedAttendArgs& a, const TileRange& t, uint
   tile.page = known ? entry : 0u;
   return tile;
 }
-// The page of the run that token `of` of the tile is in: in RUN == 16 the entry of any of the run's tokens that is looked up will do.
-template <uint32_t RUN>
-__device__ inline uint32_t page_of(const Tile& t, uint32_t run) {
-  if constexpr (RUN == 32u) return (uint32_t)__builtin_amdgcn_readfirstlane((int)t.page);
-  const uint32_t mine = t.counted >> (16u * run) & 0xFFFFu;
-  return (uint32_t)__builtin_amdgcn_readlane((int)t.page, (int)(16u * run + (mine ? (uint32_t)__builtin_ctz(mine) : 0u)));
-}
-
-// Where the rows of a tile's tokens are read from: 16 bytes at a time, from a place that is the same for all lanes and 32 bits of a lane's own (runs),
-// or an address a lane (single tokens).
+// Where the rows of a tile's tokens are read from, 16 bytes at a time: from a place that is the same for all lanes and 32 bits of a lane's own, or an address
+// a lane.
 template <uint32_t RUN>
 struct RowSource {
-  const uint8_t* base[RUN == 16u ? 2 : 1];
-  __device__ inline RowSource(const PagedAttendArgs& a, const uint8_t* pool, const Tile& t) {
-    if constexpr (RUN == 1u) {
-      base[0] = pool;
-    } else {
-      const uint64_t in_page = (uint64_t)(t.first & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride;
-#pragma unroll
-      for (uint32_t r = 0; r < 32u / RUN; ++r) base[r] = pool + (uint64_t)page_of<RUN>(t, r) * a.p.page_stride + (RUN == 32u ? in_page : 0u);
-    }
+  const uint8_t* base;
+  __device__ inline RowSource(const PagedAttendArgs& a, const uint8_t* pool, const Tile& t) : base(pool) {
+    if constexpr (RUN == 32u)
+      base += (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)t.page) * a.p.page_stride +
+              (uint64_t)(t.first & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride;
   }
-  // token `of` = fixed + own (fixed: the same for all lanes, with own within one run)
-  __device__ inline const uint8_t* row(const PagedAttendArgs& a, const Tile& t, uint32_t fixed, uint32_t own, uint32_t piece) const {
-    if constexpr (RUN == 1u) {
-      const uint32_t page = (uint32_t)__shfl((int)t.page, (int)(fixed + own));
-      return base[0] + (uint64_t)page * a.p.page_stride + (uint64_t)((t.first + fixed + own) & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride + piece;
-    } else {
-      return base[RUN == 16u ? fixed / 16u : 0u] + ((fixed % RUN + own) * (uint32_t)a.p.token_stride + piece);
-    }
+  __device__ inline const uint8_t* row(const PagedAttendArgs& a, const Tile& t, uint32_t of, uint32_t piece) const {
+    if constexpr (RUN == 32u) return base + (of * (uint32_t)a.p.token_stride + piece);
+    const uint32_t page = (uint32_t)__shfl((int)t.page, (int)of);
+    return base + (uint64_t)page * a.p.page_stride + (uint64_t)((t.first + of) & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride + piece;
   }
 };
 
@@ -187,7 +171,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
       const RowSource<RUN> from(a, keys, t);
 #pragma unroll
       for (uint32_t h = 0; h < 2u; ++h) {
-        const uint8_t* p = from.row(a, t, h * 16u, n, g * 16u);
+        const uint8_t* p = from.row(a, t, h * 16u + n, g * 16u);
 #pragma unroll
         for (uint32_t k = 0; k < kSteps; ++k) kx[h][k] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + k * 64u));
       }
@@ -195,7 +179,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
     const auto load_values = [&](const Tile& t) {
       const RowSource<RUN> from(a, values, t);
 #pragma unroll
-      for (uint32_t j = 0; j < kLoads; ++j) vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from.row(a, t, j * kRowsAtOnce, lane / kRowLanes, (lane % kRowLanes) * 16u)));
+      for (uint32_t j = 0; j < kLoads; ++j) vx[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from.row(a, t, j * kRowsAtOnce + lane / kRowLanes, (lane % kRowLanes) * 16u)));
     };
     TileRange range = tile_range(seen, from);
     uint32_t entry = look_up<RUN>(a, row, range, lane);
@@ -380,8 +364,9 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a,
   if (at == 0u) tops[threadIdx.x / kLanes] = (f32x2){m, l};
   __syncthreads();
   if (group != 0u || !some) return;
+  const uint32_t busy = min(groups, last - first + 1u);                // groups that have a part
 #pragma unroll 4
-  for (uint32_t k = 1; k < groups; ++k) {
+  for (uint32_t k = 1; k < busy; ++k) {
     const f32x2 ml = tops[k * together + threadIdx.x / kLanes];
     const float top = fmaxf(m, ml.x);
     const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top), take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);
@@ -403,18 +388,21 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a,
 template <typename T, int D>
 hipError_t launch_attend_of(const PagedAttendArgs& a, bool may_split, hipStream_t stream) {
   const uint32_t items = a.p.rows * a.p.kv_heads * a.blocks;
-  const uint32_t grid = (a.most + kAttendWaves - 1u) / kAttendWaves;         // teams, or waves in fours
+  const uint32_t grid = (a.most + kAttendWaves - 1u) / kAttendWaves;
+  // Pages that hold whole tiles: 64 rows of 1004 seen tokens 31.8 us, an address a lane 33.0; 131071 tokens 96.4, 97.1.  A third way, halves of a tile by page, was
+  // no faster than an address a lane with pages of 16 (151.5 us each for 48 rows of up to 8K tokens).
   if (a.p.page_shift >= 5u) attend_kernel<T, D, 32u><<<grid, kAttendThreads, 0, stream>>>(a);
-  else if (a.p.page_shift == 4u) attend_kernel<T, D, 16u><<<grid, kAttendThreads, 0, stream>>>(a);
   else attend_kernel<T, D, 1u><<<grid, kAttendThreads, 0, stream>>>(a);
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && may_split) {
-    // Many parts an item (a long sequence among few): many threads for each head; otherwise one workgroup for an item's heads.
-    const uint32_t heads = std::min(16u, a.rep);
-    if (a.most / items >= 64u) {
+    // The more parts an item has, the more threads a head: 1024, 256, or one workgroup for an item's heads.  131071 tokens, 256 parts: 96 us, with the small
+    // workgroups 118; 1500 tokens, 47 parts: 11.2, with 1024 threads a head 12.5, with all heads in a workgroup 14; 16 rows of 1500, 16 parts: 19.7, 23.5,
+    // 21.6; 64 rows with 4 parts: 31.6 together, 36.7 with 256 a head.
+    const uint32_t heads = std::min(16u, a.rep), parts = a.most / items;
+    if (parts >= 64u) {
       attend_join_kernel<D, 1024><<<dim3(items, heads), 1024, 0, stream>>>(a, 1u);
     } else {
-      const uint32_t together = std::min(heads, 256u / (D / 4u));
+      const uint32_t together = parts >= 8u ? 1u : std::min(heads, 256u / (D / 4u));
       attend_join_kernel<D, 256><<<dim3(items, (heads + together - 1u) / together), 256, 0, stream>>>(a, together);
     }
     e = hipGetLastError();
