@@ -131,7 +131,7 @@ struct PromptPlan {
 int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
   if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
   a.rep = (uint32_t)(q_heads / p->kv_heads);
-  // 128 dimensions: tiles of 256 pairs (8 waves) where there is one for every CU (an 8K prompt 566 us, with tiles of 128 626; six short prompts 21.8, 17.5).
+  // 128 dimensions: tiles of 256 pairs (8 waves) where there is one for every CU (an 8K prompt 571 us, with tiles of 128 619; six short prompts 21.4, 17.4).
   // 64 dimensions do better with three workgroups of 4 waves a CU (170 us, 198), 256 have no registers for two waves a SIMD.
   a.waves = p->head_dim == 128 && tokens * q_heads >= 256 * 256 ? 8u : 4u;
   a.per = 32u * a.waves / a.rep;

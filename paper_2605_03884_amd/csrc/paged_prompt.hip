@@ -1,20 +1,25 @@
 // paged_prompt.hip — attention of many new tokens of every sequence over its pages: each sees what stands up to its own place, with a window
 // the last `window` tokens and the first `sinks`.
 //
-// Work: a workgroup takes a tile of (query token, query head) pairs of one kv head, 32 a wave, so that a key is read once for all query heads that
-// share it, and goes through the keys they see 64 at a time, with a running maximum m, sum l and sum of p.V.  Where there are few query
-// tiles the keys are split as well, and a second kernel joins the parts.
+// Work: a workgroup of 4 or 8 waves takes a tile of (query token, query head) pairs of one kv head, 32 a wave, so that a key is read once for all query
+// heads that share it, and goes through the keys they see, 32 or 64 at a time, with a running maximum m, sum l and sum of p.V.  Where there are few query tiles
+// the keys are split as well, and a second kernel joins the parts.
 //
-// A tile of 64 keys, one wave (lane = 32 h + n; n is the lane's pair):
-//   staging  rows of K and V go from memory into registers and on into LDS, K two tiles ahead of its use and V one, each into one of two
-//            places.
-//   scores   S^T = K Q^T on v_mfma_f32_32x32x16: a lane gets 32 scores of its own pair.
+// A tile of keys, one wave (lane = 32 h + n; n is the lane's pair):
+//   staging  rows of K and V go from memory into registers and on into LDS, K three tiles ahead of its use and V two; entries are looked up a tile before that.
+//   scores   S^T = K Q^T on v_mfma_f32_32x32x16, 32 keys at a time: a lane gets 16 scores of its own pair, the lane 32 further on the other 16.
 //   softmax  in the lane, and with the lane 32 further on.  m follows the true maximum only when that has grown by 2^8: sums are
 //            kept relative to m, and the weights have 2^7 of room below and 2^8 above before fp16 could overflow.
 //   values   O^T = V^T P^T: the weights are where the product wants them; V^T comes out of LDS through the transposing read.
-// The scores of a tile are worked out while the weights of the tile before are (matrix and vector units side by side), its maximum
-// while the product of the tile before is.
+// The scores of the next 32 keys are worked out while the weights of these are (matrix and vector units side by side), their maximum while
+// the product with the values is.
 // The weights are rounded to the cache's type, as the result is: their errors average out over the keys and stay at the size of the result's own rounding.
+//
+// What bounds it: the chip's power where everything is busy.  8192 tokens of 32 heads, 128 dimensions: 566 - 584 us, 940 - 970 TFLOP/s, where a product of 8192^3 reaches
+// 1256 alone; matrix units are busy 50 % of the cycles, vector instructions issue in 47 %, and the clock falls from 2.3 to 1.8 GHz.  64 dimensions have
+// half the matrix work for as many weights: a window of 1024 over 2 x 8000 tokens of 32 heads takes 172 us, vector instructions issuing in 63 % of the cycles.  61
+// tokens behind 32768: 66 us, of which 10 join 32 parts.  Scores beside weights brought the 8K prompt from 675 to 609 us, LDS rows that meet each bank once and reads
+// six matrix instructions ahead of their use 593, masks as bits 584.
 #include "paged.h"
 #include "paged_values.h"
 #include "qkv_common.h"
@@ -31,7 +36,7 @@ __device__ inline float uniform(float x) { return __builtin_bit_cast(float, __bu
 // Rows of K and V in LDS are longer than they need to be, by 16 and 64 bytes: 16 lanes that read a piece of 16 bytes of as many rows of K, and 32 that
 // read 64 bytes of four rows of V through the transposing read, then meet every bank once.
 
-// Keys of a tile: as many as leave LDS for two workgroups of 4 waves a CU, or one of 8.
+// Keys of a tile: as many as leave LDS for two workgroups of 4 waves a CU, or one of 8.  Workgroups of 8 waves go through 64 as two halves between two barriers.
 constexpr uint32_t prompt_keys(uint32_t waves) { return waves == 8u ? 64u : 32u; }
 // Waves a SIMD holds at once: what its 512 registers allow.
 constexpr uint32_t prompt_waves_a_simd(int D) { return D == 256 ? 1u : D == 128 ? 2u : 3u; }
@@ -458,7 +463,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   }
 }
 
-// Joins the parts of the query heads of one token, D / 4 lanes each.
+// Joins the parts of the query heads of one token, D / 4 lanes each: 32 parts of 61 tokens of 32 heads, 32 MB, 10.5 us (3 TB/s, two rounds of reads).
 constexpr uint32_t kJoinThreads = 256;
 
 template <typename T, int D, uint32_t KEYS>
@@ -512,6 +517,7 @@ __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptAr
   if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+// Pages that hold a whole tile, pages that hold 16 rows, others: 8K prompt with pages of 64 tokens 571 us, 577 by runs of 16, 584 by an address a thread.
 template <typename T, int D, uint32_t WAVES>
 void launch_prompt_run(const PagedPromptArgs& a, hipStream_t stream) {
   const dim3 grid(places(a.tokens, a.p.rows, a.per) * a.p.kv_heads, a.splits);
