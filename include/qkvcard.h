@@ -588,7 +588,9 @@ int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspa
  * Attention over the pages of one layer.  With R = q_heads / kv_heads (at most QKV_PAGED_MAX_REP) query head hq reads kv head hq / R; a query
  * at place p of its sequence sees the tokens t <= p and, with window > 0, of those only t > p - window and t < sinks:
  *     s_t = softmax_scale * <q, K_t>,   out = sum_t softmax(s)_t * V_t,   lse = log sum_t exp(s_t)
- * A query that sees nothing has out = 0, lse = -inf.  Tokens that are not seen count for nothing, whatever their rows hold.
+ * A query that sees nothing has out = 0, lse = -inf.  Tokens that are not seen count for nothing, whatever their rows hold.  Of those that are seen, one with
+ * a score of -inf weighs nothing, a value that is infinite or no number makes its own dimension of out one; a head with a score that is +inf or no number has
+ * unspecified results.
  *   q_dev:    device, values of the pages' type: query i, head hq start i * q_token_stride + hq * q_head_stride elements behind it; strides
  *             multiples of 8, 16-byte aligned, so a part of a fused projection's result will do.
  *   lse_dev:  device, float [tokens][q_heads], may be NULL.
@@ -605,6 +607,8 @@ int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspa
  * [tokens][q_heads][head_dim]; weights are rounded to that type for the product with the values, sums and lse are fp32.  out and lse of tokens
  * behind the last row's are left as they were; a row with more new tokens than length is QKV_STATUS_BAD_ROW (those in front see nothing).
  *
+ * Limits: tokens * q_heads < 2^31; with G = ceil(R / 16) rows * kv_heads * G < 2^22 and rows * kv_heads * G * (row_pages * page_tokens / 32 + 3) < 2^31 for
+ * qkv_paged_attend; with P = 128 / R, rounded down, (tokens / P + rows) * kv_heads < 2^23 for qkv_paged_prompt.
  * Errors: QKV_ERR_NULL, QKV_ERR_SHAPE (also: window < 0, sinks without a window, a scale that is not finite), QKV_ERR_ALIGN,
  * QKV_ERR_CAPACITY, QKV_ERR_HIP.
  */

@@ -235,6 +235,76 @@ def test_batches_that_make_no_sense_stay_inside():
         assert int(cache.status) == qkv.STATUS_BAD_ROW, starts
 
 
+@pytest.mark.parametrize("rows", [63, 64, 65])
+def test_rows_around_a_wave(rows):
+    new = [(i * 5) % 4 for i in range(rows - 1)] + [9]
+    cache = Cache([n + i % 40 for i, n in enumerate(new)], 1, 64, 16, seed=rows)
+    got = run(cache, new, 2, 64, 0.125)
+    check(cache, new, got, expected(cache, new, got[0], 0.125), 64)
+    assert int(cache.status) == 0
+
+
+def test_rows_that_share_pages_and_queries_that_share_values():
+    """Two rows with the same pages, all heads with the same query (strides of 0): every result stands twice, for each head of a kv head."""
+    cache = Cache([0, 700], 2, 128, 16, seed=31)
+    cache.glens[0], cache.gtable[0] = 700, cache.gtable[1]
+    x = torch.randn(14, 128, generator=torch.Generator().manual_seed(1)).half()
+    x[7:] = x[:7]
+    q = x.cuda()[:, None].expand(14, 8, 128)
+    starts = torch.tensor([0, 7, 14], dtype=torch.int32, device="cuda")
+    out, lse = torch.empty(14, 8, 128, dtype=torch.float16, device="cuda"), torch.empty(14, 8, device="cuda")
+    qkv.paged_prompt(cache.pages, q, starts, 0.09, out, lse)
+    assert torch.equal(out[:7], out[7:]) and torch.equal(lse[:7], lse[7:])
+    for h in range(8):
+        assert torch.equal(out[:, h], out[:, h // 4 * 4]) and torch.equal(lse[:, h], lse[:, h // 4 * 4])
+    want = paged_ref.attend(x[:7].double().numpy()[:, None].repeat(8, 1), *cache.rows()[1], list(range(693, 700)), 0.09, 0, 0, ())
+    check_prompt(out[:7].double().cpu().numpy(), lse[:7].double().cpu().numpy(), want, 128, 700, "fp16", float(np.abs(cache.rows()[1][1]).max()))
+
+
+@pytest.mark.parametrize("new,old", [([5, 2], [3000, 1500]), ([80, 33], [40, 0])])
+def test_in_a_graph_whose_lengths_change(new, old):
+    """Captured once (with parts, where few queries stand behind many keys), replayed while lengths, starts and queries change, with eager calls in between."""
+    cache = Cache([a + b + 40 for a, b in zip(new, old)], 2, 128, 16, seed=33)
+    tokens = sum(new)
+    q = torch.randn(tokens, 8, 128, generator=torch.Generator().manual_seed(2)).half().cuda()
+    starts = torch.tensor([0, new[0], tokens], dtype=torch.int32, device="cuda")
+    workspace = torch.empty(qkv.paged_prompt_workspace(cache.pages, 8, tokens), dtype=torch.uint8, device="cuda")
+    other = torch.empty_like(workspace)
+    out, lse = torch.empty_like(q), torch.empty(tokens, 8, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        qkv.paged_prompt(cache.pages, q, starts, 0.09, out, lse, workspace=workspace, status=cache.status)
+    for step in range(4):
+        cache.glens.copy_(torch.tensor([a + b + 13 * step for a, b in zip(new, old)], dtype=torch.int32))
+        starts[1] = new[0] - step // 2
+        q.mul_(-1.0)
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        graph.replay()
+        eager, eager_lse = torch.empty_like(q), torch.empty_like(lse)
+        qkv.paged_prompt(cache.pages, q, starts, 0.09, eager, eager_lse, workspace=other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.equal(lse, eager_lse), step
+    assert int(cache.status) == 0
+
+
+def test_two_streams_at_once():
+    cache = Cache([4000, 900], 2, 128, 64, seed=35)
+    q = torch.randn(12, 8, 128, generator=torch.Generator().manual_seed(2)).half().cuda()
+    starts = torch.tensor([0, 7, 12], dtype=torch.int32, device="cuda")
+    want, _ = qkv.paged_prompt(cache.pages, q, starts, 0.09, torch.empty_like(q))
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(q) for _ in range(2)]
+    spaces = [torch.empty(qkv.paged_prompt_workspace(cache.pages, 8, 12), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    for _ in range(20):
+        for stream, out, space in zip(streams, outs, spaces):
+            with torch.cuda.stream(stream):
+                qkv.paged_prompt(cache.pages, q, starts, 0.09, out, workspace=space)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
 def test_without_lse_the_same_bits():
     cache = Cache([200], 2, 128, 16, seed=9)
     _, a, _ = run(cache, [150], 8, 128, 0.1)
