@@ -117,10 +117,10 @@ QKV_HD KeyTiles key_tiles_of(int32_t base, uint32_t here, int32_t window, int32_
   k.tiles = k.head + (stop > k.body ? stop - k.body : 0u);
   return k;
 }
-// Parts the keys of a query tile are cut into: as many as there may be, of at least 512 keys (six prompts of up to 450 keys 17.4 us, with 256 keys a part 20.3; 61 tokens
+// Parts the keys of a query tile are cut into: as many as there may be, of at least `least` keys (512 where there are few query tiles: six prompts of up to 450 keys 17.4 us, with 256 keys a part 20.3; 61 tokens
 // behind 32768 take 67 - 69 with 256, 512 or 1024).
-QKV_HD uint32_t prompt_splits(uint32_t keys, uint32_t most) {
-  const uint32_t n = keys / 512u;
+QKV_HD uint32_t prompt_splits(uint32_t keys, uint32_t most, uint32_t least = 512u) {
+  const uint32_t n = keys / least;
   return n < 2u ? 1u : n < most ? n : most;
 }
 
@@ -181,7 +181,7 @@ struct PagedPromptArgs {
   uint8_t* out;
   float* lse;
   float *part_o, *part_ml;                               // [splits][tokens][q heads][dim], [...][2]
-  uint32_t splits;
+  uint32_t splits, least;                                // parts of a query tile's keys at most, keys of a part at least
   uint32_t* status;
 };
 

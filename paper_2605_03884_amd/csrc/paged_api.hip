@@ -125,7 +125,7 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
 }
 
 struct PromptPlan {
-  uint32_t rep, per, waves, splits;
+  uint32_t rep, per, waves, splits, least;
   uint64_t floats;
 };
 int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
@@ -139,11 +139,25 @@ int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPla
   if (tiles * a.waves * 64u >= (1ull << 32)) return QKV_ERR_SHAPE;       // threads of a grid's dimension
   // Few query tiles: the keys are split until there are two workgroups to a CU, where sequences turn out to have that many (61 tokens of 32 heads behind
   // 32768: 16 parts 75 us, 32 65, 64 87 while their join still took a fifth longer).  Tiles of 256 pairs are never so few.
-  const uint64_t room = prompt_splits((uint32_t)p->row_pages * (uint32_t)p->page_tokens + 128u, 64u);
-  uint64_t n = 512u / (uint64_t)((tokens + a.per - 1) / a.per * p->kv_heads);
-  if (a.waves == 8u) n = 1u;
-  if (n > room) n = room;
-  a.splits = n < 2u ? 1u : (uint32_t)n;
+  const uint64_t room = (uint64_t)p->row_pages * (uint64_t)p->page_tokens + 128u, groups = (uint64_t)((tokens + a.per - 1) / a.per) * (uint64_t)p->kv_heads;
+  a.least = 512u;
+  a.splits = a.waves == 8u || groups > 256u ? 1u : prompt_splits((uint32_t)room, groups > 8u ? (uint32_t)(512u / groups) : 64u);
+  // Workgroups that leave much of the chip idle at the end (264 where 256 run at once): up to four long parts, until they fill 82 % of its turns, from where on the
+  // power is what counts; each part costs a few percent to write and to join.  32 heads of 128 dimensions behind 32768 tokens: 1100 tokens 1004 us -> 787, 2100
+  // 1900 -> 1370, 4500 3280 -> 2845; behind 16000 503 -> 404, 934 -> 690, 1625 -> 1493, with parts of at least 8192 keys 504, 773, 1499; with parts of
+  // 2048, 4500 tokens with nothing in front 201 -> 242.  Where sequences turn out to be short, the join's look at them is 1 - 2 us.
+  const uint64_t at_once = p->head_dim == 64 ? 768u : p->head_dim == 128 && a.waves == 4u ? 512u : 256u;
+  if (a.splits == 1u && groups > 256u && groups < 4u * at_once) {
+    a.least = 4096u;
+    double best = 0.0;
+    for (uint64_t n = 1; n <= 4u && (n == 1u || n * a.least <= room); ++n) {
+      const double turns = (double)(groups * n) / (double)at_once, worth = std::fmin(turns / std::ceil(turns), 0.82) - 0.025 * (double)(n - 1u);
+      if (worth > best) {
+        best = worth;
+        a.splits = (uint32_t)n;
+      }
+    }
+  }
   a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
   return QKV_OK;
 }
@@ -323,6 +337,7 @@ int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   a.part_o = static_cast<float*>(query->workspace_dev);
   a.part_ml = plan.floats ? a.part_o + plan.splits * (uint64_t)query->tokens * (uint64_t)query->q_heads * (uint64_t)pages->head_dim : nullptr;
   a.splits = plan.splits;
+  a.least = plan.least;
   a.status = query->status_dev;
   return launch_paged_prompt(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? QKV_OK : QKV_ERR_HIP;

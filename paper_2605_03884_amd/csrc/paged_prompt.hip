@@ -3,7 +3,7 @@
 //
 // Work: a workgroup of 4 or 8 waves takes a tile of (query token, query head) pairs of one kv head, 32 a wave, so that a key is read once for all query
 // heads that share it, and goes through the keys they see, 32 or 64 at a time, with a running maximum m, sum l and sum of p.V.  Where there are few query tiles
-// the keys are split as well, and a second kernel joins the parts.
+// the keys are split as well, and where their number would leave much of the chip idle at the end; a second kernel joins the parts.
 //
 // A tile of keys, one wave (lane = 32 h + n; n is the lane's pair):
 //   staging  rows of K and V go from memory into registers and on into LDS, K three tiles ahead of its use and V two; entries are looked up a tile before that.
@@ -108,7 +108,7 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   const KeyTiles key_tiles = key_tiles_of(base, here, window, sinks, kKeys);
   const int32_t win_lo = key_tiles.win_lo;
   const uint32_t sink_end = key_tiles.sink_end, head = key_tiles.head, body = key_tiles.body, tiles = key_tiles.tiles;
-  const uint32_t splits = prompt_splits(tiles * kKeys, a.splits);
+  const uint32_t splits = prompt_splits(tiles * kKeys, a.splits, a.least);
   if (blockIdx.y >= splits) return;
   const uint32_t first_tile = (uint32_t)((uint64_t)tiles * blockIdx.y / splits), last_tile = (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / splits);
   const auto tile_at = [&](uint32_t i) -> int32_t { return (int32_t)((i < head ? i : body + (i - head)) * kKeys); };
@@ -466,55 +466,57 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
 // Joins the parts of the query heads of one token, D / 4 lanes each: 32 parts of 61 tokens of 32 heads, 32 MB, 10.5 us (3 TB/s, two rounds of reads).
 constexpr uint32_t kJoinThreads = 256;
 
-template <typename T, int D, uint32_t KEYS>
+template <typename T, int D>
 __global__ __launch_bounds__(kJoinThreads) void prompt_join_kernel(PagedPromptArgs a) {
   constexpr uint32_t kLanes = D / 4, kAtOnce = 8;
-  const uint32_t lane = threadIdx.x % kWaveSize, q_heads = a.p.kv_heads * a.rep, token = blockIdx.x;
+  const uint32_t lane = threadIdx.x % kWaveSize, q_heads = a.p.kv_heads * a.rep, token = blockIdx.x, keys = prompt_keys(a.waves);
   const uint32_t row = (uint32_t)__builtin_amdgcn_readfirstlane((int)find_row(a.p.rows, lane, [&](uint32_t b) { return (uint32_t)a.starts[b] <= token; }));
   const int32_t start = a.starts[row], end = a.starts[row + 1u];
   if (start < 0 || (uint32_t)start > token || end <= (int32_t)token || (uint32_t)end > a.tokens) return;      // nobody's token has no parts
   const uint32_t count = (uint32_t)(end - start), skip = (token - (uint32_t)start) / a.per * a.per;
   const int32_t length = (int32_t)held(a.p.lens[row], a.p.row_pages, a.p.page_shift);
-  const KeyTiles key_tiles = key_tiles_of(length - (int32_t)count + (int32_t)skip, min(a.per, count - skip), (int32_t)a.window, (int32_t)min(a.sinks, 0x7FFFFFFFu), KEYS);
-  const uint32_t splits = prompt_splits(key_tiles.tiles * KEYS, a.splits);
+  const KeyTiles key_tiles = key_tiles_of(length - (int32_t)count + (int32_t)skip, min(a.per, count - skip), (int32_t)a.window, (int32_t)min(a.sinks, 0x7FFFFFFFu), keys);
+  const uint32_t splits = prompt_splits(key_tiles.tiles * keys, a.splits, a.least);
   if (splits == 1u) return;                                            // finished where it was
-  const uint32_t hq = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes, at = threadIdx.x % kLanes;
-  if (hq >= q_heads) return;
-  const uint64_t all = (uint64_t)a.tokens * q_heads, pair = (uint64_t)token * q_heads + hq;
-  float m = -INFINITY, l = 0.0f;
-  f32x4 o = (f32x4)(0.0f);
-  for (uint32_t s = 0; s < splits; s += kAtOnce) {
-    f32x2 ml[kAtOnce];
-    f32x4 x[kAtOnce];
+  const uint32_t at = threadIdx.x % kLanes;
+  const uint64_t all = (uint64_t)a.tokens * q_heads;
+  for (uint32_t hq = blockIdx.y * (kJoinThreads / kLanes) + threadIdx.x / kLanes; hq < q_heads; hq += gridDim.y * (kJoinThreads / kLanes)) {
+    const uint64_t pair = (uint64_t)token * q_heads + hq;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = (f32x4)(0.0f);
+    for (uint32_t s = 0; s < splits; s += kAtOnce) {
+      f32x2 ml[kAtOnce];
+      f32x4 x[kAtOnce];
 #pragma unroll
-    for (uint32_t k = 0; k < kAtOnce; ++k) {
-      const uint64_t slot = min(s + k, splits - 1u) * all + pair;      // past the last one: the last one, without weight
-      ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
-      x[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
-    }
-    float top = m;
+      for (uint32_t k = 0; k < kAtOnce; ++k) {
+        const uint64_t slot = min(s + k, splits - 1u) * all + pair;      // past the last one: the last one, without weight
+        ml[k] = *reinterpret_cast<const f32x2*>(a.part_ml + slot * 2u);
+        x[k] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + at * 4u);
+      }
+      float top = m;
 #pragma unroll
-    for (uint32_t k = 0; k < kAtOnce; ++k) {
-      if (s + k >= splits) ml[k].x = -INFINITY;
-      top = fmaxf(top, ml[k].x);
-    }
-    const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top);
-    l *= keep;
-    o *= keep;
+      for (uint32_t k = 0; k < kAtOnce; ++k) {
+        if (s + k >= splits) ml[k].x = -INFINITY;
+        top = fmaxf(top, ml[k].x);
+      }
+      const float keep = m == -INFINITY ? 0.0f : exp2f_(m - top);
+      l *= keep;
+      o *= keep;
 #pragma unroll
-    for (uint32_t k = 0; k < kAtOnce; ++k) {
-      const float take = ml[k].x == -INFINITY ? 0.0f : exp2f_(ml[k].x - top);
-      l += ml[k].y * take;
-      o += x[k] * take;
+      for (uint32_t k = 0; k < kAtOnce; ++k) {
+        const float take = ml[k].x == -INFINITY ? 0.0f : exp2f_(ml[k].x - top);
+        l += ml[k].y * take;
+        o += x[k] * take;
+      }
+      m = top;
     }
-    m = top;
+    const float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
+    typename T::x4 r;
+#pragma unroll
+    for (uint32_t e = 0; e < 4u; ++e) r[e] = (typename T::one)(o[e] * scale);
+    *reinterpret_cast<typename T::x4*>(a.out + (pair * D + at * 4u) * 2u) = r;
+    if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
-  const float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-  typename T::x4 r;
-#pragma unroll
-  for (uint32_t e = 0; e < 4u; ++e) r[e] = (typename T::one)(o[e] * scale);
-  *reinterpret_cast<typename T::x4*>(a.out + (pair * D + at * 4u) * 2u) = r;
-  if (a.lse && at == 0u) a.lse[pair] = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 // Pages that hold a whole tile, pages that hold 16 rows, others: 8K prompt with pages of 64 tokens 571 us, 577 by runs of 16, 584 by an address a thread.
@@ -532,7 +534,9 @@ hipError_t launch_prompt_of(const PagedPromptArgs& a, hipStream_t stream) {
   else launch_prompt_run<T, D, 4u>(a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1u) return e;
-  prompt_join_kernel<T, D, prompt_keys(4u)><<<dim3(a.tokens, (a.p.kv_heads * a.rep + kJoinThreads / (D / 4) - 1u) / (kJoinThreads / (D / 4))), kJoinThreads, 0, stream>>>(a);
+  // Long parts come with many tokens, and with none at all where sequences turn out to be short: a workgroup a token, which goes through its heads.
+  const uint32_t groups = a.least > 512u ? 1u : (a.p.kv_heads * a.rep + kJoinThreads / (D / 4) - 1u) / (kJoinThreads / (D / 4));
+  prompt_join_kernel<T, D><<<dim3(a.tokens, groups), kJoinThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -289,6 +289,26 @@ def test_in_a_graph_whose_lengths_change(new, old):
     assert int(cache.status) == 0
 
 
+@pytest.mark.parametrize("kind,dim,new,old,q_heads,heads,window", [("fp16", 128, [2100], [17000], 32, 8, 0), ("bf16", 256, [2100], [25000], 16, 8, 0),
+                                                                   ("fp16", 64, [1500, 2, 0, 2700], [16500, 33000, 9, 100], 16, 8, 0),
+                                                                   ("bf16", 128, [1100], [24000], 32, 8, 17000)])
+def test_workgroups_that_would_leave_the_chip_idle(kind, dim, new, old, q_heads, heads, window):
+    """Long keys in a few parts behind many queries, short sequences among them whole: some tokens of each row against the definition."""
+    cache = Cache([a + b for a, b in zip(new, old)], heads, dim, 64, kind, seed=41)
+    space = qkv.paged_prompt_workspace(cache.pages, q_heads, sum(new) + 3)
+    assert space >= 2 * (sum(new) + 3) * q_heads * (dim + 2) * 4
+    q, out, lse = run(cache, new, q_heads, dim, dim ** -0.5, window=window, sinks=5 if window else 0)
+    at = 0
+    for b, (K, V) in enumerate(cache.rows()):
+        pick = sorted({0, 1, new[b] // 2, new[b] - 130, new[b] - 2, new[b] - 1} & set(range(new[b])))
+        if pick:
+            mine = [at + i for i in pick]
+            want = paged_ref.attend(q[mine].double().numpy(), K, V, [old[b] + i for i in pick], dim ** -0.5, window, 5 if window else 0)
+            check_prompt(out[mine], lse[mine], want, dim, cache.lens[b], kind, float(np.abs(V).max()))
+        at += new[b]
+    assert np.isfinite(out).all() and np.isfinite(lse).all() and int(cache.status) == 0
+
+
 def test_two_streams_at_once():
     cache = Cache([4000, 900], 2, 128, 64, seed=35)
     q = torch.randn(12, 8, 128, generator=torch.Generator().manual_seed(2)).half().cuda()
