@@ -1,4 +1,5 @@
 """ctypes marshalling for the C ABI declared in include/qkvcard.h (same names, same order)."""
+import contextlib
 import ctypes
 import os
 
@@ -268,6 +269,13 @@ def _stream(stream):
     return stream.cuda_stream
 
 
+def _scratch(nbytes, device, stream):
+    """Device memory for a call that brings none of its own.  It is given back when the call returns, so it is taken from the memory of the stream
+    the call runs on: whoever gets it next is queued behind the call's work, and the call behind whoever had it before."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _dev_ptr(t, dtype=None, name="tensor"):
     if not t.is_cuda:
         raise ValueError("%s must live in device memory" % name)
@@ -482,7 +490,7 @@ def card_attend(card, expect, q, softmax_scale, out, lse=None, workspace=None, s
     n = card.numel() if card_nbytes is None else int(card_nbytes)
     q_heads = q.shape[1]
     if workspace is None:
-        workspace = torch.empty(card_attend_workspace(expect, q_heads), dtype=torch.uint8, device=card.device)
+        workspace = _scratch(card_attend_workspace(expect, q_heads), card.device, stream)
     lp = _optional_ptr(lse, torch.float32, "lse")
     sp = _optional_ptr(status, None, "status")
     _check(lib().qkv_card_attend(_dev_ptr(card, torch.uint8, "card"), n, ctypes.byref(expect),
@@ -498,7 +506,7 @@ def card_attend_kc(card, expect, q, softmax_scale, out, lse=None, workspace=None
     n = card.numel() if card_nbytes is None else int(card_nbytes)
     q_heads = q.shape[1]
     if workspace is None:
-        workspace = torch.empty(card_attend_workspace(expect, q_heads), dtype=torch.uint8, device=card.device)
+        workspace = _scratch(card_attend_workspace(expect, q_heads), card.device, stream)
     lp = _optional_ptr(lse, torch.float32, "lse")
     sp = _optional_ptr(status, None, "status")
     _check(lib().qkv_card_attend_kc(_dev_ptr(card, torch.uint8, "card"), n, ctypes.byref(expect),
@@ -609,7 +617,7 @@ def pages_compact_workspace(pages):
 def pages_compact(pages, status, live=None, workspace=None, stream=None):
     """Moves the pages in use to the front of the pool; live: device int32 [1] for their number, or None."""
     if workspace is None:
-        workspace = torch.empty(pages_compact_workspace(pages), dtype=torch.uint8, device=pages.device)
+        workspace = _scratch(pages_compact_workspace(pages), pages.device, stream)
     lp = None if live is None else _of_pages(live, pages, torch.int32, (1,), "live")
     _check(lib().qkv_pages_compact(pages, lp, _of_pages(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel(),
                                    _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_compact")
@@ -642,7 +650,7 @@ def paged_attend(pages, q, softmax_scale, out, lse=None, layer=0, window=0, sink
     rows is fine); out: device float32 of the same shape; lse: float32 [rows, q_heads]; prior: (out, lse) of attention over other tokens
     (card_attend's), which the result then covers too."""
     if workspace is None:
-        workspace = torch.empty(paged_attend_workspace(pages, q.shape[1]), dtype=torch.uint8, device=pages.device)
+        workspace = _scratch(paged_attend_workspace(pages, q.shape[1]), pages.device, stream)
     x = _paged_query(pages, q, softmax_scale, out, torch.float32, lse, layer, window, sinks, workspace, status)
     if prior is not None:
         x.prior_out_dev = _of_pages(prior[0], pages, torch.float32, q.shape, "prior[0]")
@@ -661,7 +669,7 @@ def paged_prompt(pages, q, starts, softmax_scale, out, lse=None, layer=0, window
     """Attention of the rows' last tokens, those of row i at q[starts[i]:starts[i + 1]], each over what stands up to its own place.
     q: device [tokens, q_heads, head_dim] of the pages' type; starts: device int32 [rows + 1]; out: of the pages' type; lse: float32 [tokens, q_heads]."""
     if workspace is None:
-        workspace = torch.empty(paged_prompt_workspace(pages, q.shape[1], q.shape[0]), dtype=torch.uint8, device=pages.device)
+        workspace = _scratch(paged_prompt_workspace(pages, q.shape[1], q.shape[0]), pages.device, stream)
     x = _paged_query(pages, q, softmax_scale, out, pages.dtype, lse, layer, window, sinks, workspace, status)
     x.starts_dev = _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
     _check(lib().qkv_paged_prompt(pages, x, _here(pages, stream)), "qkv_paged_prompt")
