@@ -150,6 +150,7 @@ struct AppendArgs {
   uint64_t layer_stride, head_stride, token_stride;      // bytes, of the new rows
   const int32_t* starts;                                 // or null: one token a row
   uint32_t tokens, layer_begin, layer_count;
+  uint32_t first;                                        // of the tokens a launch takes
   uint32_t* status;
 };
 

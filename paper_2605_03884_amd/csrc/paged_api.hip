@@ -186,6 +186,7 @@ int qkv_pages_append(const qkv_pages_t* pages, const qkv_rows_t* rows, uint32_t*
   a.tokens = (uint32_t)rows->tokens;
   a.layer_begin = (uint32_t)rows->layer_begin;
   a.layer_count = (uint32_t)rows->layer_count;
+  a.first = 0u;
   a.status = status_dev;
   return launch_pages_append(cache_of(pages), a, static_cast<hipStream_t>(stream)) == hipSuccess ? QKV_OK : QKV_ERR_HIP;
 }

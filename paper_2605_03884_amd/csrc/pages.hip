@@ -4,6 +4,8 @@
 // All bookkeeping runs on the device, on whole numbers whose result does not hang on the order of the threads: pages are
 // given out lowest first, in the order of the rows.  What decides (reserve, the allocation of a fork, the plan of a
 // compaction) is one workgroup; what moves bytes is spread over the chip.
+#include <algorithm>
+
 #include "paged.h"
 #include "qkv_common.h"
 
@@ -22,11 +24,13 @@ constexpr uint32_t kPicked = 4096;          // free pages a plan looks up at a t
 // difference).  One token of 64 rows: 3.7.
 constexpr uint32_t kAppendThreads = 256;
 constexpr uint32_t kAppendBlock = 4;
+constexpr uint32_t kAppendLaunch = 1u << 25;             // tokens of a launch: 2^31 threads, where a grid's dimension holds fewer than 2^32
+static_assert(kAppendLaunch % kAppendBlock == 0 && (uint64_t)kAppendLaunch / kAppendBlock * kAppendThreads < (1ull << 32));
 
 __global__ __launch_bounds__(kAppendThreads) void append_kernel(PageCache c, AppendArgs a) {
   __shared__ uint64_t to[kAppendBlock];                    // byte offset of the token's row in head 0, or ~0
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
-  const uint32_t first = blockIdx.x * kAppendBlock, count = min(kAppendBlock, a.tokens - first);
+  const uint32_t first = a.first + blockIdx.x * kAppendBlock, count = min(kAppendBlock, a.tokens - first);
   const bool values = (blockIdx.y & 1u) != 0u;
   const uint32_t layer = blockIdx.y >> 1;
   for (uint32_t i = wave; i < count; i += kAppendThreads / kWaveSize) {
@@ -370,10 +374,15 @@ __global__ __launch_bounds__(kRowThreads) void compact_move_kernel(PageCache c, 
 }  // namespace
 
 hipError_t launch_pages_append(const PageCache& c, const AppendArgs& a, hipStream_t stream) {
-  if (a.tokens == 0u) return hipSuccess;
-  const dim3 grid((a.tokens + kAppendBlock - 1u) / kAppendBlock, 2u * a.layer_count);
-  append_kernel<<<grid, kAppendThreads, 0, stream>>>(c, a);
-  return hipGetLastError();
+  AppendArgs some = a;
+  for (some.first = 0u; some.first < a.tokens; some.first += kAppendLaunch) {
+    const uint32_t tokens = std::min(a.tokens - some.first, kAppendLaunch);
+    const dim3 grid((tokens + kAppendBlock - 1u) / kAppendBlock, 2u * a.layer_count);
+    append_kernel<<<grid, kAppendThreads, 0, stream>>>(c, some);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_pages_reserve(const PageCache& c, const int32_t* more, uint32_t* status, hipStream_t stream) {
