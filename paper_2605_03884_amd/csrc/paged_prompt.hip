@@ -306,7 +306,8 @@ __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void pro
   const auto follow = [&](f32x16& s) {
     const float most = max32(top) * scale;
     if (__builtin_amdgcn_ballot_w64(most > m + slack) != 0ull) {
-      if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(most) > kFar) != 0ull && (special & kScaled) == 0u) {
+      // a pair that sees none of these keys has a maximum of -inf, which is not far: its weights are 0 whatever is rounded
+      if (__builtin_amdgcn_ballot_w64(__builtin_fabsf(most) > kFar && most != -INFINITY) != 0ull && (special & kScaled) == 0u) {
         s *= scale;
         scale = uniform(1.0f);
         slack = uniform(0.0f);
