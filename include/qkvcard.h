@@ -595,7 +595,8 @@ int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspa
  *             multiples of 8, 16-byte aligned, so a part of a fused projection's result will do.
  *   lse_dev:  device, float [tokens][q_heads], may be NULL.
  *   workspace_dev: device scratch, 16-byte aligned, contents unspecified, of the bytes the call's _workspace function names; NULL where
- *             that is 0.  Two calls that may run at once, graphs among them, need one each.
+ *             that is 0.  Two calls that may run at once, graphs among them, need one each.  What qkv_paged_prompt_workspace names for a
+ *             number of tokens is enough for every batch of that pool and q_heads with as many tokens or fewer.
  *
  * qkv_paged_attend: one new token of every sequence, p = lens_dev[i] - 1; tokens == rows, starts_dev NULL.  out is float
  * [rows][q_heads][head_dim], 16-byte aligned.  prior_out / prior_lse (float, shapes of out / lse, both or neither): the result of

@@ -660,6 +660,7 @@ def paged_attend(pages, q, softmax_scale, out, lse=None, layer=0, window=0, sink
 
 
 def paged_prompt_workspace(pages, q_heads, tokens):
+    """Bytes that are enough for every batch of up to `tokens` tokens."""
     out = ctypes.c_uint64(0)
     _check(lib().qkv_paged_prompt_workspace(pages, int(q_heads), int(tokens), ctypes.byref(out)), "qkv_paged_prompt_workspace")
     return out.value

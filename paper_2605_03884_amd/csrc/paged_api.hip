@@ -1,4 +1,5 @@
 // paged_api.hip — the C ABI of the cache in pages: argument checks and launch planning.
+#include <algorithm>
 #include <cmath>
 
 #include "paged.h"
@@ -124,6 +125,9 @@ int plan_attend(const qkv_pages_t* p, int32_t q_heads, AttendPlan& a) {
   return QKV_OK;
 }
 
+constexpr int64_t kLargePrompt = 256 * 256;      // (token, query head) pairs
+constexpr uint64_t kMostCut = 4u * 768u;         // query tiles from which on keys are never cut
+
 struct PromptPlan {
   uint32_t rep, per, waves, splits, least;
   uint64_t floats;
@@ -133,7 +137,7 @@ int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPla
   a.rep = (uint32_t)(q_heads / p->kv_heads);
   // 128 dimensions: tiles of 256 pairs (8 waves) where there is one for every CU (an 8K prompt 571 us, with tiles of 128 619; six short prompts 21.4, 17.4).
   // 64 dimensions do better with three workgroups of 4 waves a CU (170 us, 198), 256 have no registers for two waves a SIMD.
-  a.waves = p->head_dim == 128 && tokens * q_heads >= 256 * 256 ? 8u : 4u;
+  a.waves = p->head_dim == 128 && tokens * q_heads >= kLargePrompt ? 8u : 4u;
   a.per = 32u * a.waves / a.rep;
   const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
   if (tiles * a.waves * 64u >= (1ull << 32)) return QKV_ERR_SHAPE;       // threads of a grid's dimension
@@ -146,7 +150,7 @@ int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPla
   // power is what counts; each part costs a few percent to write and to join.  32 heads of 128 dimensions behind 32768 tokens: 1100 tokens 1004 us -> 787, 2100
   // 1900 -> 1370, 4500 3280 -> 2845; behind 16000 503 -> 404, 934 -> 690, 1625 -> 1493, with parts of at least 8192 keys 504, 773, 1499; with parts of
   // 2048, 4500 tokens with nothing in front 201 -> 242.  Where sequences turn out to be short, the join's look at them is 1 - 2 us.
-  const uint64_t at_once = p->head_dim == 64 ? 768u : p->head_dim == 128 && a.waves == 4u ? 512u : 256u;
+  const uint64_t at_once = p->head_dim == 64 ? 768u : p->head_dim == 128 && a.waves == 4u ? 512u : 256u;      // kMostCut / 4 at most
   if (a.splits == 1u && groups > 256u && groups < 4u * at_once) {
     a.least = 4096u;
     double best = 0.0;
@@ -159,6 +163,24 @@ int plan_prompt(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPla
     }
   }
   a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
+  return QKV_OK;
+}
+
+// The most that any batch of up to `tokens` tokens needs.  It is not the largest one that needs it: parts get fewer as query tiles get more.  With a number of
+// query tiles given the batch that fills them needs most; behind kMostCut of them none has parts.
+int most_prompt_floats(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, uint64_t& floats) {
+  PromptPlan plan;
+  const int rc = plan_prompt(p, q_heads, tokens, plan);
+  if (rc) return rc;
+  floats = plan.floats;
+  const int64_t large = p->head_dim == 128 ? (kLargePrompt + q_heads - 1) / q_heads : INT64_MAX;      // batches from here on have tiles of 8 waves
+  for (uint32_t waves = 4u; waves <= plan.waves; waves += 4u) {
+    const int64_t last = waves == 4u ? std::min(tokens, large - 1) : tokens, per = 32u * waves / plan.rep;
+    for (int64_t n = per; n - per < last && (uint64_t)(n / per) * (uint64_t)p->kv_heads < kMostCut; n += per) {
+      PromptPlan smaller;
+      if (plan_prompt(p, q_heads, std::min(n, last), smaller) == QKV_OK) floats = std::max(floats, smaller.floats);
+    }
+  }
   return QKV_OK;
 }
 
@@ -299,10 +321,10 @@ int qkv_paged_prompt_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_
   if (rc) return rc;
   rc = check_heads(pages, q_heads);
   if (rc) return rc;
-  PromptPlan plan;
-  rc = plan_prompt(pages, q_heads, tokens, plan);
+  uint64_t floats = 0;
+  rc = most_prompt_floats(pages, q_heads, tokens, floats);
   if (rc) return rc;
-  *bytes_out = plan.floats * sizeof(float);
+  *bytes_out = floats * sizeof(float);
   return QKV_OK;
 }
 
