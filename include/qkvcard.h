@@ -601,7 +601,8 @@ int qkv_pages_compact(const qkv_pages_t* pages, int32_t* live_dev, void* workspa
  * qkv_paged_attend: one new token of every sequence, p = lens_dev[i] - 1; tokens == rows, starts_dev NULL.  out is float
  * [rows][q_heads][head_dim], 16-byte aligned.  prior_out / prior_lse (float, shapes of out / lse, both or neither): the result of
  * attention over tokens that are somewhere else, qkv_card_attend's over a card above all; out and lse are then those of both together.
- * (prior_out may be out itself, and prior_lse lse.)  All sums in fp32, weights held to 22 bits or more.
+ * (prior_out may be out itself, and prior_lse lse.)  All sums in fp32; weights held to 22 bits, in fp16 those
+ * below 2^-18 of the largest to 2^-40 of it.
  *
  * qkv_paged_prompt: many new tokens, whose keys and values are in the pages already: token i of row b (starts_dev as for qkv_pages_append,
  * here required, tokens >= 1) stands at place lens_dev[b] - n_b + (i - starts_dev[b]).  out is of the pages' type,

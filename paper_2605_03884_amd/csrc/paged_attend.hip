@@ -15,8 +15,8 @@
 //            follows); V^T wants 4 tokens of one dimension in a lane, which the transposing read of LDS gives.
 //            Rows of V stand in LDS with their 32-byte pieces exchanged by token, so that neither side meets a bank twice.
 // The sum of a head that sees anything is at least 1, so the hardware's reciprocal and logarithm, which know no subnormals, serve (1 step each).
-// The weights are held to 22 bits (fp16: high part and remainder; bf16, 8 bits each, high part and two remainders), scaled by 2^10 so that
-// what fp16 loses below 2^-14 counts for nothing; maxima, sums and results are in 32 bits.
+// The weights are held to 22 bits (fp16: high part and remainder; bf16, 8 bits each, high part and two remainders, 24 bits), in fp16 scaled by 2^15: those
+// below 2^-18 of the largest lose bits, and are off by 2^-40 of it at most, 2^-23 over 131072 of them.  Maxima, sums and results are in 32 bits.
 //
 // What bounds it: memory, and the chain lengths - entries - K, V - two tiles where little is read.  48 rows of up to 8192 tokens, 8 kv heads of 128 dimensions: 152 us, 146 of
 // them here (5.8 TB/s; reads alone reach 6.9), 131071 tokens of one row 92 - 96 with 84 here (6.4 TB/s); 37 tokens 6.4 - 8.  Loads that pass the
@@ -33,7 +33,6 @@ namespace {
 
 constexpr uint32_t kAttendThreads = 256;
 constexpr uint32_t kAttendWaves = kAttendThreads / kWaveSize;
-constexpr float kLift = 10.0f;                           // weights are 2^kLift times what they are
 
 __device__ inline uint32_t sum64(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_readlane((int)wave_inclusive_scan(x), 63);
@@ -239,7 +238,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
       for (uint32_t j = 1; j < 8u; ++j) top = fmaxf(top, e[j]);
       top = max32(max16(top));
       const float m_new = fmaxf(m, top);
-      const float less = m_new == -INFINITY ? 0.0f : m_new - kLift;    // what is taken off in the exponent
+      const float less = m_new == -INFINITY ? 0.0f : m_new - T::kLift; // what is taken off in the exponent
       if (__builtin_amdgcn_ballot_w64(m_new != m) != 0ull) {
         const float shrink = m == -INFINITY ? 0.0f : exp2f_(m - m_new);
         l *= shrink;
@@ -274,11 +273,44 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
+    // Values that are infinite or no number.  Their products are whatever the parts of a weight make of them (0 times infinity is no number), so a dimension
+    // that they have spoilt becomes their sum, whatever they weigh; what no such value has spoilt, a weight has, and stays.
+    f32x4 zero = (f32x4)(0.0f);                                        // stays that only where all are numbers
+#pragma unroll
+    for (uint32_t d = 0; d < kSlabs; ++d) zero += acc[d] * 0.0f;
+    const bool spoilt = !(zero.x + zero.y + zero.z + zero.w == 0.0f);
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(spoilt) != 0ull, 0)) {
+      f32x4 odd[kSlabs];
+#pragma unroll
+      for (uint32_t d = 0; d < kSlabs; ++d) odd[d] = (f32x4)(0.0f);
+      const int32_t* entries = a.p.table + (uint64_t)row * a.p.row_pages;
+      for (uint32_t i = from; i < upto; ++i) {
+        const TileRange t = tile_range(seen, i);
+        for (uint32_t token = t.lo; token < t.hi; ++token) {
+          const uint32_t page = (uint32_t)entries[token >> a.p.page_shift];
+          if (page >= a.p.pages) continue;
+          const uint8_t* p = values + (uint64_t)page * a.p.page_stride + (uint64_t)(token & ((1u << a.p.page_shift) - 1u)) * a.p.token_stride + g * 8u;
+#pragma unroll
+          for (uint32_t d = 0; d < kSlabs; ++d) {
+            const typename T::x4 v = *reinterpret_cast<const typename T::x4*>(p + d * 32u);
+#pragma unroll
+            for (uint32_t j = 0; j < 4u; ++j)
+              if (!(__builtin_fabsf((float)v[j]) < INFINITY)) odd[d][j] += (float)v[j];
+          }
+        }
+      }
+#pragma unroll
+      for (uint32_t d = 0; d < kSlabs; ++d)
+#pragma unroll
+        for (uint32_t j = 0; j < 4u; ++j)
+          if (!(__builtin_fabsf(odd[d][j]) < INFINITY)) acc[d][j] = odd[d][j];
+    }
+
     l = sum32(sum16(l));
     if (from == 0u && upto == tiles) {                                 // the whole item
       const uint64_t at_head = (uint64_t)row * q_heads + hq;
       float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-      float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+      float lse = m == -INFINITY ? -INFINITY : (m - T::kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
       float other = 0.0f;
       if (n < heads) {
         if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
@@ -314,7 +346,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
 // Joins the parts of an item that was cut: a workgroup takes `together` query heads of one item, D / 4 lanes each, and goes through the
 // parts in as many groups of those lanes as it has.
 template <int D, uint32_t THREADS>
-__global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a, uint32_t together) {
+__global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a, uint32_t together, float lift) {
   constexpr uint32_t kLanes = D / 4, kAtOnce = 4;
   __shared__ f32x4 sums[THREADS];
   __shared__ f32x2 tops[THREADS / kLanes];
@@ -381,7 +413,7 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a,
   }
   const uint64_t at_head = (uint64_t)row * q_heads + (inner / a.blocks) * a.rep + block * 16u + in_block;
   float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
-  float lse = m == -INFINITY ? -INFINITY : (m - kLift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  float lse = m == -INFINITY ? -INFINITY : (m - lift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   float other = 0.0f;
   if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
   o *= scale;
@@ -405,10 +437,10 @@ hipError_t launch_attend_of(const PagedAttendArgs& a, bool may_split, hipStream_
     // 21.6; 64 rows with 4 parts: 31.6 together, 36.7 with 256 a head.
     const uint32_t heads = std::min(16u, a.rep), parts = a.most / items;
     if (parts >= 64u) {
-      attend_join_kernel<D, 1024><<<dim3(items, heads), 1024, 0, stream>>>(a, 1u);
+      attend_join_kernel<D, 1024><<<dim3(items, heads), 1024, 0, stream>>>(a, 1u, T::kLift);
     } else {
       const uint32_t together = parts >= 8u ? 1u : std::min(heads, 256u / (D / 4u));
-      attend_join_kernel<D, 256><<<dim3(items, (heads + together - 1u) / together), 256, 0, stream>>>(a, together);
+      attend_join_kernel<D, 256><<<dim3(items, (heads + together - 1u) / together), 256, 0, stream>>>(a, together, T::kLift);
     }
     e = hipGetLastError();
   }

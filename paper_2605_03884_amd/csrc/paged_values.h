@@ -69,14 +69,16 @@ struct Half {
   static constexpr uint32_t kParts = 2;
   static __device__ inline f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ inline f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
-  // e as a sum of parts, each cut off towards zero but the last, which is rounded.  No part is 0: an infinite value stays infinite in
-  // the product with each of them (what that adds, 2^-24 at most where a weight of 1 is 2^10, is below the sums' last bit).
+  // Weights are 2^kLift times what they are, the largest 2^15 (2^16 where a maximum's own steps are larger than that): a part's last bit is 2^-24 at the
+  // smallest, 2^-39 of the largest weight.
+  static constexpr float kLift = 15.0f;
+  // e, at most 2^16, as a sum of parts: the first one cut off towards zero, which stops at 65504, the rest rounded.
   static __device__ inline void parts(const float (&e)[8], x8 (&w)[kParts]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const h16x2 high = __builtin_amdgcn_cvt_pkrtz(fmaxf(e[j], 0x1p-24f), 0.0f);
+      const h16x2 high = __builtin_amdgcn_cvt_pkrtz(e[j], 0.0f);
       w[0][j] = (_Float16)high[0];
-      w[1][j] = (_Float16)fmaxf(e[j] - (float)w[0][j], 0x1p-24f);
+      w[1][j] = (_Float16)(e[j] - (float)w[0][j]);
     }
   }
 };
@@ -89,14 +91,15 @@ struct BFloat {
   static constexpr uint32_t kParts = 3;
   static __device__ inline f32x4 mfma16(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ inline f32x16 mfma32(x8 a, x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+  static constexpr float kLift = 0.0f;                   // parts reach as far down as e itself does
   static __device__ inline void parts(const float (&e)[8], x8 (&w)[kParts]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float high = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, e[j]) & 0xFFFF0000u), rest = e[j] - high;
       const float middle = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, rest) & 0xFFFF0000u), low = rest - middle;
-      w[0][j] = (__bf16)fmaxf(high, 0x1p-60f);
-      w[1][j] = (__bf16)fmaxf(middle, 0x1p-60f);
-      w[2][j] = (__bf16)fmaxf(low, 0x1p-60f);
+      w[0][j] = (__bf16)high;
+      w[1][j] = (__bf16)middle;
+      w[2][j] = (__bf16)low;
     }
   }
 };
