@@ -390,8 +390,8 @@ __global__ __launch_bounds__(THREADS) void attend_join_kernel(PagedAttendArgs a,
     o *= keep;
 #pragma unroll
     for (uint32_t k = 0; k < kAtOnce; ++k) {
-      if (ml[k].x == -INFINITY) continue;                              // such a part may hold anything
-      const float take = exp2f_(ml[k].x - top);
+      if (s + k * groups > last) continue;
+      const float take = ml[k].x == -INFINITY ? 0.0f : exp2f_(ml[k].x - top);      // no weight, but what is infinite in it is seen
       l += ml[k].y * take;
       o += x[k] * take;
     }

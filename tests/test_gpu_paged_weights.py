@@ -114,3 +114,22 @@ def test_infinite_values_reach_their_dimension_whatever_they_weigh(kind, lens, h
         assert (np.abs(got[b] - out[0])[~hit] <= bound[0][~hit]).all()
         assert np.isfinite(lse[b]).all()
     assert int(cache.status) == 0
+
+
+@pytest.mark.parametrize("lens,heads", [([5000], 1), ([40, 3000, 900], 2), ([100], 1)])
+def test_an_infinite_value_among_tokens_that_all_weigh_nothing(lens, heads):
+    """A part of a cut sequence in which every score is -inf: its values that are infinite or no number are seen all the same."""
+    cache = Cache(lens, heads, 64, 32, seed=3, strong=1.0)
+    for b, n in enumerate(lens):
+        for token in range(n // 2 // 32 * 32, n // 2 // 32 * 32 + 32):
+            if token < n - 1:
+                page, place = int(cache.table[b, token // 32]), token % 32
+                cache.k[0, page, :, place, 0] = -float("inf")
+                if token % 32 == 5:
+                    cache.v[0, page, :, place, 9] = float("inf")
+    cache.gpu()
+    q = torch.randn(len(lens), heads, 64, generator=torch.Generator().manual_seed(1)).half()
+    q[..., 0] = 1.0
+    got, lse = run(cache, q, 0.125)
+    assert not np.isfinite(got[..., 9]).any() and np.isfinite(lse).all()
+    assert np.isfinite(np.delete(got, 9, -1)).all()
