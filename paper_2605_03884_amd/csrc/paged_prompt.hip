@@ -29,7 +29,9 @@ namespace {
 
 constexpr float kLift = 7.0f, kSlack = 8.0f;
 // From here on a maximum's rounding counts in an exponent that is not rounded: scores are multiplied with the scale by themselves, and m follows at once.
-constexpr float kFar = 0x1p20f;
+// A wave's pairs change over together.  Where one of them has a smaller maximum its scores were not rounded up to there and are afterwards, which may set
+// equal ones apart by half a step: 2^-13 at most, a fraction of what rounding a weight to 16 bits does.
+constexpr float kFar = 0x1p12f;
 constexpr uint32_t kLost = 1u, kScaled = 2u;             // what a wave has met: an entry that names no page, a maximum beyond kFar
 __device__ inline float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 
