@@ -273,6 +273,9 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
+    // No load is on its way any more, which the compiler cannot see: it would wait for them, and with them for this item's stores, where the next item begins.
+    __builtin_amdgcn_s_waitcnt(0x0F70);                                // vmcnt(0)
+
     // Values that are infinite or no number.  Their products are whatever the parts of a weight make of them (0 times infinity is no number), so a dimension
     // that they have spoilt becomes their sum, whatever they weigh; what no such value has spoilt, a weight has, and stays.
     f32x4 zero = (f32x4)(0.0f);                                        // stays that only where all are numbers
