@@ -15,11 +15,12 @@
 // the product with the values is.
 // The weights are rounded to the cache's type, as the result is: their errors average out over the keys and stay at the size of the result's own rounding.
 //
-// What bounds it: the chip's power where everything is busy.  8192 tokens of 32 heads, 128 dimensions: 561 - 589 us, 930 - 980 TFLOP/s, where a product of 8192^3 reaches
-// 1256 alone; matrix units are busy 46 % of the cycles, vector instructions issue in 44 %, and the clock falls from 2.3 to 1.8 GHz.  64 dimensions have
-// half the matrix work for as many weights: a window of 1024 over 2 x 8000 tokens of 32 heads takes 171 us, vector instructions issuing in 53 % of the cycles, matrix units busy 25 %.  61
-// tokens behind 32768: 66 us, of which 10 join 32 parts.  Scores beside weights brought the 8K prompt from 675 to 609 us, LDS rows that meet each bank once and reads
-// six matrix instructions ahead of their use 593, masks as bits 584.
+// What bounds it: no one unit where everything is busy.  8192 tokens of 32 heads, 128 dimensions: 550 - 600 us, 920 - 1000 TFLOP/s, where a product of 8192^3 reaches
+// 1256 alone; matrix units are busy 46 % of the cycles, vector instructions issue in 44 %, and the clock, cycles over time, is 1.8 - 2.0 GHz.  64 dimensions have
+// half the matrix work for as many weights: a window of 1024 and four sinks over 8000 and 3711 tokens of 32 heads takes 164 - 173 us, vector instructions issuing in 55 % of the
+// cycles (7 a weight), matrix units busy 26 %.  The same window without sinks, whose first keys not all pairs of a wave see, over 8000 and 7000 tokens: 64 dimensions 372 - 390 us for
+// 64 heads, 128 dimensions 349 - 376 for 32.  61 tokens behind 32768: 64 - 67 us, of which 10 join 32 parts.  Scores beside weights brought the 8K prompt from 675 to 609 us, LDS rows that meet
+// each bank once and reads six matrix instructions ahead of their use 593, masks as bits 584.
 #include "paged.h"
 #include "paged_values.h"
 #include "qkv_common.h"

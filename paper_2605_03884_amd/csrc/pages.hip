@@ -91,7 +91,8 @@ __device__ inline uint32_t block_scan(uint32_t x, uint32_t* waves, uint32_t& tot
 }
 
 // The bookkeeping kernels are bound by the latency of their steps: a pass over refs is a trip to memory for 4096 pages, a scan two barriers.  24 forks
-// take 4.5 us to release, 4.8 to plan, and 21 to copy 127 MB (6 TB/s).
+// take 4.5 us to release, 5 to plan, and 21 - 23 to copy 127 MB (5.5 - 6 TB/s).  Room for 64 rows that each cross a page: 6 us in a pool of 4096 pages,
+// 84 in a nearly full one of 100000.
 //
 // Gives out pages: want(i) of them to item i < items, lowest free page first, in the items' order; give(i, j, page) takes the
 // j-th page of item i.  Nothing is given out unless all can be.  One workgroup; refs are changed by give().
@@ -307,7 +308,7 @@ __global__ __launch_bounds__(kRowThreads) void free_kernel(PageCache c, const in
 //
 // With n pages in use, the k-th page in use at n or above goes to the k-th free page below n: sources and destinations are
 // apart, so all moves may run at once.  A page's rank is how many pages in use lie below it; `kept` pages in use lie below n, so the
-// movers have the ranks kept .. n - 1.  Memory bounds the moves: 0.84 GB of pages 340 us at worst, 5 TB/s read and written, behind 4.8 us of planning.  Workspace: {moves, n, kept, -}, the holes, the movers by rank, the ranks by page.
+// movers have the ranks kept .. n - 1.  Memory bounds the moves: 0.84 GB of pages 337 - 348 us, 4.9 TB/s read and written, behind 4.9 us of planning.  Workspace: {moves, n, kept, -}, the holes, the movers by rank, the ranks by page.
 __global__ __launch_bounds__(kPlanThreads) void compact_plan_kernel(PageCache c, int32_t* live_out, int32_t* work, uint32_t* status) {
   __shared__ uint32_t waves[kPlanThreads / kWaveSize];
   uint32_t mine = 0u, live;
