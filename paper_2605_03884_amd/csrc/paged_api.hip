@@ -1,6 +1,7 @@
 // paged_api.hip — the C ABI of the cache in pages: argument checks and launch planning.
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "paged.h"
 
@@ -96,9 +97,10 @@ uint64_t most_tiles(const qkv_pages_t* p) { return ((uint64_t)p->row_pages * (ui
 // A window that holds any sequence the table has room for is none.
 uint32_t window_of(const qkv_pages_t* p, int32_t window) { return (int64_t)window >= (int64_t)p->row_pages * p->page_tokens ? 0u : (uint32_t)window; }
 
-// The scale for powers of two.  One of 0 is as good as none, but infinity times it has to stay infinite.
+// The scale for powers of two.  One of 0 is as good as none, but infinity times it has to stay infinite, as 0 times the largest has to stay 0.
 float scale_of(float scale) {
-  const float x = (float)((double)scale * 1.4426950408889634);
+  const double most = std::numeric_limits<float>::max();
+  const float x = (float)std::min(std::max((double)scale * 1.4426950408889634, -most), most);
   return std::fabs(x) >= 1e-37f ? x : x < 0.0f ? -1e-37f : 1e-37f;
 }
 

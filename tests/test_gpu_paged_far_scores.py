@@ -95,3 +95,19 @@ def test_prompts(kind, scale, order, new, old, heads, q_heads, dim, size):
         pick = list(range(new[b])) if new[b] < 200 else list(range(0, new[b], 61)) + [new[b] - 1]
         mine = [starts[b] + i for i in pick]
         check(out[mine], lse[mine], leaders(j[b], V, [old[b] + i for i in pick]), q0[mine], scale, q_heads, HALF_STEP[kind], lens[b])
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("scale", [3.4e38, -3.4e38, 2.4e38])
+def test_the_largest_scales_leave_scores_of_zero_what_they_are(kind, scale):
+    """A product of 0 scores 0, whatever the scale: all tokens weigh the same."""
+    cache = Cache([90, 700], 1, 64, 16, kind, seed=5)
+    q = torch.zeros(2, 2, 64, dtype=TYPES[kind])
+    out, lse = torch.empty(2, 2, 64, device="cuda"), torch.empty(2, 2, device="cuda")
+    qkv.paged_attend(cache.pages, q.cuda(), scale, out, lse)
+    half, half_lse = torch.empty(2, 2, 64, dtype=TYPES[kind], device="cuda"), torch.empty(2, 2, device="cuda")
+    qkv.paged_prompt(cache.pages, q.cuda(), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"), scale, half, half_lse)
+    for b, (_, V) in enumerate(cache.rows()):
+        want = (V.mean(1).repeat(2, 0)[None], np.abs(V).mean(1).repeat(2, 0)[None], np.zeros(1), np.array([cache.lens[b]], dtype=np.float64))
+        check(out[b:b + 1].double().cpu().numpy(), lse[b:b + 1].double().cpu().numpy(), want, np.zeros((1, 2)), 1.0, 2, 0.0, cache.lens[b])
+        check(half[b:b + 1].double().cpu().numpy(), half_lse[b:b + 1].double().cpu().numpy(), want, np.zeros((1, 2)), 1.0, 2, HALF_STEP[kind], cache.lens[b])
