@@ -560,9 +560,10 @@ int qkv_pages_append(const qkv_pages_t* pages, const qkv_rows_t* rows, uint32_t*
 
 /*
  * Sequences that go on from another one: row target_dev[i] becomes what row source_dev[i] is (device, int32_t[count], 1 <= count <= rows).
- * What the targets held is given back first.  Full pages are shared; a last page that is not full is copied (its tokens, in all layers) to a
- * new page, the lowest free one, in the order of the pairs.  Targets are all different and none is a source, else
- * QKV_STATUS_BAD_ROW; with too few free pages QKV_STATUS_NO_PAGES; in both cases nothing has changed when the call's work is done.
+ * What the targets held is given back first.  Full pages are shared: tokens that a source has room for are written before it is forked.  A last
+ * page that is not full is copied (its tokens, in all layers) to a new page, the lowest free one, in the order of the pairs.  Targets are all
+ * different and none is a source, else QKV_STATUS_BAD_ROW; with too few free pages QKV_STATUS_NO_PAGES; in both cases nothing has changed when
+ * the call's work is done.
  */
 int qkv_pages_fork(const qkv_pages_t* pages, const int32_t* source_dev, const int32_t* target_dev, int32_t count, uint32_t* status_dev,
                    void* stream);

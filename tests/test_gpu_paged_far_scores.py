@@ -1,7 +1,8 @@
 """Attention over pages with scores of up to 2^32 that are known exactly: the tokens with the largest score share all the weight.
 
 One dimension of q and K carries whole numbers, so that products of q and K are exact in fp32; two different ones are at least 8 apart, times a scale of 2^8 or more.
-The weight of a token is 1 / (how many have the largest score) or nothing, however a score of 2^20 or 2^30 is rounded: equal ones are rounded alike."""
+The weight of a token is 1 / (how many have the largest score) or nothing, however a score of 2^20 or 2^30 is rounded: equal ones are rounded alike,
+or half a step apart where that is 2^-13 at most (a prompt's scores, where a wave begins to round them)."""
 import numpy as np
 import pytest
 import torch
