@@ -281,7 +281,7 @@ __global__ __launch_bounds__(kAttendThreads, D == 256 ? 1 : 2) void attend_kerne
     f32x4 zero = (f32x4)(0.0f);                                        // stays that only where all are numbers
 #pragma unroll
     for (uint32_t d = 0; d < kSlabs; ++d) zero += acc[d] * 0.0f;
-    const bool spoilt = !(zero.x + zero.y + zero.z + zero.w == 0.0f);
+    const bool spoilt = n < heads && !(zero.x + zero.y + zero.z + zero.w == 0.0f);      // (places without a query head meet infinite keys with zeros)
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(spoilt) != 0ull, 0)) {
       f32x4 odd[kSlabs];
 #pragma unroll
