@@ -641,6 +641,109 @@ int qkv_paged_prompt_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_
 int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, void* stream);
 
 /*
+ * Attention over pages that a cheap score chooses for each query: where sequences are long - a whole injected context in front of the receiver's own
+ * tokens (paper Sec. 4.2.2) - most pages weigh next to nothing for a given query.  Three steps, each a call:
+ *   qkv_pages_digest           bounds of the keys of a page, once, when it has been filled
+ *   qkv_paged_choose           the pages of every (query token, kv head), from those bounds
+ *   qkv_paged_attend_chosen,   qkv_paged_attend and qkv_paged_prompt over the chosen pages
+ *   qkv_paged_prompt_chosen
+ *
+ * A digest of a page, for one layer and kv head: per channel d an upper bound of its keys' values, then (head_dim further on) a lower one, as codes of the
+ * step 2^e(d):
+ *     hi(d) = sat8(ceil(max_t K_t(d) * 2^-e(d))),   lo(d) = sat8(floor(min_t K_t(d) * 2^-e(d))),   sat8: to -128 .. 127
+ * A channel in which a key is no number has 127 and -128.  The steps are the caller's, the same for all pages of a layer, for instance for every channel
+ * the smallest e with max |K(d)| <= 127 * 2^e over the first prompt; all int8_t values are allowed.  A digest belongs to the page: qkv_pages_fork needs
+ * nothing for the pages it shares (and a page that is copied is not full), but after qkv_pages_compact digests are to be made again.
+ *
+ * A choice is a bit for each page of a sequence, bit j % 32 of word j / 32 for its page j, [tokens][kv_heads][(row_pages + 31) / 32] words.
+ */
+typedef struct qkv_digests {
+  void* const* layers;                     /* host array [layers] of device pointers, 16-byte aligned: int8_t [pages][kv_heads][2][head_dim] */
+  const int8_t* exponents_dev;             /* device, [layers][kv_heads][head_dim], 16-byte aligned: e */
+} qkv_digests_t;
+
+/*
+ * Digests of the pages that new tokens have filled, in layers layer_begin .. layer_begin + layer_count - 1: of row b the full pages with a token among the
+ * last n_b = starts_dev[b + 1] - starts_dev[b] of its lens_dev[b] (starts_dev and tokens as for qkv_pages_append, whose call has written them; starts_dev
+ * NULL: one token for every row that has any, tokens == rows).  With n_b = lens_dev[b] that is all full pages of the row.  Digests of other pages stay.
+ * An entry that names no page is QKV_STATUS_BAD_PAGE; a row whose starts lie outside the tokens or apart by more than its length is QKV_STATUS_BAD_ROW; both
+ * are left out.  Limit: (tokens / page_tokens + rows) * kv_heads < 2^24.
+ */
+int qkv_pages_digest(const qkv_pages_t* pages, const qkv_digests_t* digests, const int32_t* starts_dev, int64_t tokens, int32_t layer_begin,
+                     int32_t layer_count, uint32_t* status_dev, void* stream);
+
+/*
+ * Chooses pages for every query token and kv head, in whole numbers, so the result hangs on no order of summation.  A query at place p of its sequence has the
+ * pages 0 .. o, o = p / page_tokens; those whose entry names no page are not there.  Of the others the first `first` (j < first) and the last `last` ones
+ * (j > o - last) are chosen, and as many more as make `most` together: those with the highest score, of equal scores the lowest j.
+ *   Query codes.  With the query heads r = 0 .. R - 1 of the kv head, in this order, in fp32:   P(d) = sum_r max(q_r(d), 0),   N(d) = sum_r min(q_r(d), 0)
+ *   (a value that is no number counts as 0; sums are held to the largest finite numbers);   x = max_d (floor(log2(max(P(d), -N(d)))) + e(d)) over the d where that is not 0;
+ *   p(d) = min(127, rne(P(d) * 2^(e(d) - x + 6))),   n(d) = max(-127, rne(N(d) * 2^(e(d) - x + 6)))    (all 0 where P and N are).
+ *   Score of page j:   sum_d p(d) hi_j(d) + n(d) lo_j(d).   But for the rounding of the codes it bounds sum_r <q_r, K_t> over the page's tokens, for a
+ *   softmax scale above 0.
+ *   q_dev, strides, tokens, starts_dev, layer, q_heads: as for qkv_paged_prompt, or with starts_dev NULL as for qkv_paged_attend.
+ *   most >= first + last, first >= 0, last >= 1: a query's own page, which need not be full, is never scored.  Digests of the full pages in front of it have to be there.
+ *   choice_dev: device, uint32_t [tokens][kv_heads][(row_pages + 31) / 32], written in full; where a query has no place (p < 0) all bits are 0.  Words of tokens behind
+ *             the last row's are left as they were.
+ *   workspace_dev: device scratch of qkv_paged_choose_workspace() bytes, 16-byte aligned, contents unspecified; NULL where that is 0.  What is named for a number
+ *             of tokens is enough for fewer.  Two calls that may run at once need one each.
+ * Limits: row_pages < 2^20; tokens * kv_heads * 64 < 2^31; for prompts (tokens / 16 + rows) * kv_heads < 2^23.
+ * Errors: QKV_ERR_NULL, QKV_ERR_SHAPE, QKV_ERR_ALIGN, QKV_ERR_CAPACITY, QKV_ERR_HIP.
+ */
+typedef struct qkv_choose {
+  const void* q_dev;
+  int64_t q_token_stride, q_head_stride;   /* in elements */
+  int64_t tokens;
+  const int32_t* starts_dev;
+  uint32_t* choice_dev;
+  void* workspace_dev;
+  uint64_t workspace_bytes;
+  uint32_t* status_dev;
+  int32_t layer, q_heads;
+  int32_t most, first, last;
+  int32_t reserved;                        /* 0 */
+} qkv_choose_t;
+
+int qkv_paged_choose_workspace(const qkv_pages_t* pages, int64_t tokens, uint64_t* bytes_out);
+int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, const qkv_choose_t* choose, void* stream);
+
+/*
+ * qkv_paged_attend and qkv_paged_prompt over chosen pages: a query at place p sees the tokens t <= p of the pages j whose bit is set.  Everything else - arguments,
+ * results, rounding, what is not seen, limits, errors - is as it is there; window and sinks are 0 (QKV_ERR_SHAPE).  Any bits will do: none, all, or a choice of the
+ * caller's own.  Bits of pages behind a query's own mean nothing, as do those behind row_pages in a last word.
+ *   choice_dev: device, uint32_t [tokens][kv_heads][(row_pages + 31) / 32].
+ *   most:     how many bits of a query are set, about; 0 if that is not known.  It guides how the work is cut, and decides with the shape how large
+ *             the workspace has to be; results are right whatever is set.
+ */
+int qkv_paged_attend_chosen_workspace(const qkv_pages_t* pages, int32_t q_heads, int32_t most, uint64_t* bytes_out);
+int qkv_paged_attend_chosen(const qkv_pages_t* pages, const qkv_paged_query_t* query, const uint32_t* choice_dev, int32_t most, void* stream);
+int qkv_paged_prompt_chosen_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_t tokens, uint64_t* bytes_out);
+int qkv_paged_prompt_chosen(const qkv_pages_t* pages, const qkv_paged_query_t* query, const uint32_t* choice_dev, void* stream);
+
+/*
+ * The maps of a ragged batch, made on the device from how many new tokens each row has: what qkv_pages_append, qkv_pages_digest, qkv_paged_choose and
+ * qkv_paged_prompt take as starts_dev, and where every token stands, for kernels of the caller's own (position embedding, a projection that writes its rows
+ * into the pages itself).  Lengths count the new tokens already (qkv_pages_reserve).
+ *   more_dev:   device, int32_t [rows]; NULL: one token for every row that has any.
+ *   tokens:     room for tokens in the maps, 1 .. 2^27 - 1.
+ *   starts_dev: device, int32_t [rows + 1], written: row b's tokens are starts_dev[b] .. starts_dev[b + 1] - 1 of the batch.
+ *   row_dev, place_dev: device, int32_t [tokens], may be NULL: the token's row and its place in the sequence.
+ *   slot_dev:   device, int64_t [tokens], 8-byte aligned, may be NULL: page * page_tokens + place % page_tokens; -1 where the entry names no page (QKV_STATUS_BAD_PAGE).
+ * Maps hold -1 behind the last row's tokens, so that a batch may be padded to a fixed size.  A number below 0 or above the row's length counts as 0; a row whose
+ * tokens do not fit has none, and neither have those behind it.  Both are QKV_STATUS_BAD_ROW.
+ */
+typedef struct qkv_slots {
+  const int32_t* more_dev;
+  int64_t tokens;
+  int32_t* starts_dev;
+  int32_t* row_dev;
+  int32_t* place_dev;
+  int64_t* slot_dev;
+} qkv_slots_t;
+
+int qkv_pages_slots(const qkv_pages_t* pages, const qkv_slots_t* slots, uint32_t* status_dev, void* stream);
+
+/*
  * Read a card's header back to the host (paper Sec. 4.2.1: the card is self-describing - sequence length, identifiers,
  * position offset, achieved average bit width) and validate it (magic, version, shape
  * domain, counts summing to tokens, section offsets equal to the closed form,

@@ -144,6 +144,41 @@ class PagedQuery(ctypes.Structure):
     ]
 
 
+class Digests(ctypes.Structure):
+    """qkv_digests_t, and the tensors it points to, which it keeps alive."""
+    _fields_ = [("layers", ctypes.POINTER(ctypes.c_void_p)), ("exponents_dev", ctypes.c_void_p)]
+
+    @classmethod
+    def make(cls, pages, layers, exponents):
+        """layers: a device int8 tensor [pages, kv_heads, 2, head_dim] for every layer of the pages; exponents: device int8 [layers, kv_heads, head_dim]."""
+        if len(layers) != pages.layers:
+            raise ValueError("digests must be one tensor for every layer of the pages")
+        shape = (pages.pages, pages.kv_heads, 2, pages.head_dim)
+        pointers = (ctypes.c_void_p * len(layers))(*[_of_pages(t, pages, torch.int8, shape, "a layer's digests") for t in layers])
+        at = _of_pages(exponents, pages, torch.int8, (pages.layers, pages.kv_heads, pages.head_dim), "exponents")
+        d = cls(ctypes.cast(pointers, ctypes.POINTER(ctypes.c_void_p)), at)
+        d.tensors = (list(layers), exponents, pointers)
+        return d
+
+
+class Choose(ctypes.Structure):
+    """qkv_choose_t."""
+    _fields_ = [
+        ("q_dev", ctypes.c_size_t), ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("tokens", ctypes.c_int64),
+        ("starts_dev", ctypes.c_size_t), ("choice_dev", ctypes.c_size_t), ("workspace_dev", ctypes.c_size_t), ("workspace_bytes", ctypes.c_uint64),
+        ("status_dev", ctypes.c_size_t), ("layer", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("most", ctypes.c_int32), ("first", ctypes.c_int32),
+        ("last", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class Slots(ctypes.Structure):
+    """qkv_slots_t."""
+    _fields_ = [
+        ("more_dev", ctypes.c_size_t), ("tokens", ctypes.c_int64), ("starts_dev", ctypes.c_size_t), ("row_dev", ctypes.c_size_t),
+        ("place_dev", ctypes.c_size_t), ("slot_dev", ctypes.c_size_t),
+    ]
+
+
 _VALUE_TYPES = {torch.float16: 0, torch.bfloat16: 1}
 
 _pointer_tables = [ctypes.c_void_p * (2 * count) for count in range(5)]
@@ -228,7 +263,15 @@ def lib():
                        ("paged_attend_workspace", [pages, ctypes.c_int32, bytes_out]),
                        ("paged_attend", [pages, ctypes.POINTER(PagedQuery), vp]),
                        ("paged_prompt_workspace", [pages, ctypes.c_int32, ctypes.c_int64, bytes_out]),
-                       ("paged_prompt", [pages, ctypes.POINTER(PagedQuery), vp])):
+                       ("paged_prompt", [pages, ctypes.POINTER(PagedQuery), vp]),
+                       ("pages_digest", [pages, ctypes.POINTER(Digests), vp, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32, vp, vp]),
+                       ("paged_choose_workspace", [pages, ctypes.c_int64, bytes_out]),
+                       ("paged_choose", [pages, ctypes.POINTER(Digests), ctypes.POINTER(Choose), vp]),
+                       ("paged_attend_chosen_workspace", [pages, ctypes.c_int32, ctypes.c_int32, bytes_out]),
+                       ("paged_attend_chosen", [pages, ctypes.POINTER(PagedQuery), vp, ctypes.c_int32, vp]),
+                       ("paged_prompt_chosen_workspace", [pages, ctypes.c_int32, ctypes.c_int64, bytes_out]),
+                       ("paged_prompt_chosen", [pages, ctypes.POINTER(PagedQuery), vp, vp]),
+                       ("pages_slots", [pages, ctypes.POINTER(Slots), vp, vp])):
         entry = getattr(L, "qkv_" + name)
         entry.restype, entry.argtypes = ctypes.c_int, args
     L.qkv_card_peek.restype = ctypes.c_int
@@ -675,3 +718,103 @@ def paged_prompt(pages, q, starts, softmax_scale, out, lse=None, layer=0, window
     x.starts_dev = _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
     _check(lib().qkv_paged_prompt(pages, x, _here(pages, stream)), "qkv_paged_prompt")
     return out, lse
+
+
+def pages_digest(pages, digests, layer=0, count=1, starts=None, tokens=None, status=None, stream=None):
+    """Digests of the pages that new tokens have filled, in layers `layer` .. `layer + count - 1`; starts: device int32 [rows + 1] and the tokens of the
+    batch (as many as starts ends with, or more), or None for one token a row."""
+    if starts is None and tokens is not None and tokens != pages.rows or starts is not None and tokens is None:
+        raise ValueError("tokens is the size of the batch that starts describes")
+    at = None if starts is None else _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
+    _check(lib().qkv_pages_digest(pages, digests, at, pages.rows if tokens is None else tokens, layer, count, _status_of_pages(status, pages), _here(pages, stream)),
+           "qkv_pages_digest")
+
+
+def _choice_shape(pages, tokens):
+    return (tokens, pages.kv_heads, (pages.row_pages + 31) // 32)
+
+
+def paged_choose_workspace(pages, tokens):
+    """Bytes that are enough for every batch of up to `tokens` tokens."""
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_paged_choose_workspace(pages, int(tokens), ctypes.byref(out)), "qkv_paged_choose_workspace")
+    return out.value
+
+
+def paged_choose(pages, digests, q, most, choice=None, first=1, last=1, layer=0, starts=None, workspace=None, status=None, stream=None):
+    """Pages for every query token and kv head, a bit each: int32 [tokens, kv_heads, (row_pages + 31) // 32], which is returned.  q: device
+    [tokens, q_heads, head_dim] of the pages' type (a view with contiguous rows is fine); starts: device int32 [rows + 1], or None for one token of every row;
+    the `first` and the `last` pages in front of a query are chosen anyway, `most` in all.  Without a choice to write to, words of tokens behind the last row's are 0."""
+    shape, strides = q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != pages.head_dim or strides[2] != 1 or q.dtype is not pages.dtype or q.device != pages.device:
+        raise ValueError("q must be [tokens, q_heads, head_dim] of the pages' type and device, rows contiguous")
+    if workspace is None:
+        workspace = _scratch(paged_choose_workspace(pages, shape[0]), pages.device, stream)
+    if choice is None:
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(stream):
+            choice = torch.zeros(_choice_shape(pages, shape[0]), dtype=torch.int32, device=pages.device)
+    x = Choose(q.data_ptr(), strides[0], strides[1], shape[0])
+    x.choice_dev = _of_pages(choice, pages, torch.int32, _choice_shape(pages, shape[0]), "choice")
+    if starts is not None:
+        x.starts_dev = _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
+    x.workspace_dev, x.workspace_bytes = _of_pages(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel()
+    x.status_dev = _status_of_pages(status, pages)
+    x.layer, x.q_heads, x.most, x.first, x.last = layer, shape[1], most, first, last
+    _check(lib().qkv_paged_choose(pages, digests, x, _here(pages, stream)), "qkv_paged_choose")
+    return choice
+
+
+def paged_attend_chosen_workspace(pages, q_heads, most=0):
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_paged_attend_chosen_workspace(pages, int(q_heads), int(most), ctypes.byref(out)), "qkv_paged_attend_chosen_workspace")
+    return out.value
+
+
+def paged_attend_chosen(pages, choice, q, softmax_scale, out, lse=None, layer=0, most=0, prior=None, workspace=None, status=None, stream=None):
+    """paged_attend over the pages whose bits are set in choice (device int32 [rows, kv_heads, (row_pages + 31) // 32], paged_choose's or any other);
+    most: about how many are, 0 if that is not known."""
+    if workspace is None:
+        workspace = _scratch(paged_attend_chosen_workspace(pages, q.shape[1], most), pages.device, stream)
+    x = _paged_query(pages, q, softmax_scale, out, torch.float32, lse, layer, 0, 0, workspace, status)
+    if prior is not None:
+        x.prior_out_dev = _of_pages(prior[0], pages, torch.float32, q.shape, "prior[0]")
+        x.prior_lse_dev = _of_pages(prior[1], pages, torch.float32, q.shape[:2], "prior[1]")
+    at = _of_pages(choice, pages, torch.int32, _choice_shape(pages, q.shape[0]), "choice")
+    _check(lib().qkv_paged_attend_chosen(pages, x, at, most, _here(pages, stream)), "qkv_paged_attend_chosen")
+    return out, lse
+
+
+def paged_prompt_chosen_workspace(pages, q_heads, tokens):
+    """Bytes that are enough for every batch of up to `tokens` tokens."""
+    out = ctypes.c_uint64(0)
+    _check(lib().qkv_paged_prompt_chosen_workspace(pages, int(q_heads), int(tokens), ctypes.byref(out)), "qkv_paged_prompt_chosen_workspace")
+    return out.value
+
+
+def paged_prompt_chosen(pages, choice, q, starts, softmax_scale, out, lse=None, layer=0, workspace=None, status=None, stream=None):
+    """paged_prompt, each token over the pages whose bits are set for it in choice (device int32 [tokens, kv_heads, (row_pages + 31) // 32])."""
+    if workspace is None:
+        workspace = _scratch(paged_prompt_chosen_workspace(pages, q.shape[1], q.shape[0]), pages.device, stream)
+    x = _paged_query(pages, q, softmax_scale, out, pages.dtype, lse, layer, 0, 0, workspace, status)
+    x.starts_dev = _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
+    at = _of_pages(choice, pages, torch.int32, _choice_shape(pages, q.shape[0]), "choice")
+    _check(lib().qkv_paged_prompt_chosen(pages, x, at, _here(pages, stream)), "qkv_paged_prompt_chosen")
+    return out, lse
+
+
+def pages_slots(pages, starts, row=None, place=None, slot=None, more=None, tokens=None, status=None, stream=None):
+    """The maps of a ragged batch from how many new tokens each row has (more: device int32 [rows]; None: one for every row that has any).  Written: starts, device
+    int32 [rows + 1]; row and place, device int32 [tokens], and slot, int64 [tokens], those that are given (without any, tokens is the room a batch has)."""
+    given = [t for t in (row, place, slot) if t is not None]
+    if given:
+        if tokens is not None and tokens != given[0].numel():
+            raise ValueError("the maps must have room for the batch's tokens")
+        tokens = given[0].numel()
+    elif tokens is None:
+        raise ValueError("without a map the room for tokens has to be given")
+    x = Slots(0 if more is None else _of_pages(more, pages, torch.int32, (pages.rows,), "more"), tokens,
+              _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts"))
+    for name, t, kind in (("row", row, torch.int32), ("place", place, torch.int32), ("slot", slot, torch.int64)):
+        if t is not None:
+            setattr(x, name + "_dev", _of_pages(t, pages, kind, (tokens,), name))
+    _check(lib().qkv_pages_slots(pages, x, _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_slots")

@@ -184,8 +184,64 @@ struct PagedPromptArgs {
   float *part_o, *part_ml;                               // [splits][tokens][q heads][dim], [...][2]
   uint32_t splits, least;                                // parts of a query tile's keys at most, keys of a part at least
   uint32_t* status;
+  const uint32_t* choice;                                // pages chosen for each (token, kv head); null where all are seen
+  uint32_t words;                                        // of one
 };
 
+struct DigestArgs {
+  const uint8_t* k[QKV_INJECT_MAX_LAYERS];               // of the layers that are digested
+  int8_t* digest[QKV_INJECT_MAX_LAYERS];
+  PageLayer p;                                           // k and v unused
+  const int8_t* exponents;                               // of the first layer that is digested
+  const int32_t* starts;                                 // or null: one token a row
+  uint32_t tokens, layers;
+  uint32_t* status;
+};
+
+struct SlotsArgs {
+  PageLayer p;
+  const int32_t* more;                                   // or null
+  uint32_t tokens;
+  int32_t *starts, *row, *place;
+  int64_t* slot;
+  uint32_t* status;
+};
+
+struct ChooseArgs {
+  PageLayer p;
+  const uint8_t* q;
+  uint64_t q_token_stride, q_head_stride;                // bytes
+  const int8_t *digest, *exponents;                      // of the layer
+  const int32_t* starts;                                 // or null: one token a row
+  uint32_t tokens, rep;
+  uint32_t per;                                          // query tokens of a tile
+  uint32_t first_tile, tiles;                            // of this launch
+  uint32_t most, first, last;
+  uint32_t words, stride;                                // of a choice; scores of a (token, kv head) in the workspace
+  uint32_t *choice, *status;
+  int32_t* scores;                                       // [tiles][per][kv heads][stride]
+};
+
+struct ChosenAttendArgs {
+  PageLayer p;
+  const uint8_t* q;
+  uint64_t q_token_stride, q_head_stride;                // bytes
+  const uint32_t* choice;
+  uint32_t words;
+  uint32_t rep, blocks;                                  // query heads per kv head, groups of 16 of them
+  uint32_t parts;                                        // workgroups of an item
+  float scale_log2, nothing;                             // as in PagedAttendArgs
+  const float *prior_out, *prior_lse;
+  float *out, *lse;
+  float *part_o, *part_ml;                               // [items][parts][heads of a block][dim], [...][2]
+  uint32_t* status;
+};
+
+hipError_t launch_pages_digest(const DigestArgs& a, uint32_t head_dim, bool bf16, hipStream_t stream);
+hipError_t launch_pages_slots(const SlotsArgs& a, hipStream_t stream);
+hipError_t launch_paged_choose(const ChooseArgs& a, uint32_t head_dim, bool bf16, hipStream_t stream);
+hipError_t launch_paged_attend_chosen(const ChosenAttendArgs& a, uint32_t head_dim, bool bf16, hipStream_t stream);
+hipError_t launch_paged_prompt_chosen(const PagedPromptArgs& a, uint32_t head_dim, bool bf16, hipStream_t stream);
 hipError_t launch_pages_append(const PageCache& c, const AppendArgs& a, hipStream_t stream);
 hipError_t launch_pages_reserve(const PageCache& c, const int32_t* more, uint32_t* status, hipStream_t stream);
 hipError_t launch_pages_fork(const PageCache& c, const int32_t* source, const int32_t* target, uint32_t n, uint32_t* status, hipStream_t stream);

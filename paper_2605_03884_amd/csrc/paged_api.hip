@@ -186,6 +186,114 @@ int most_prompt_floats(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, ui
   return QKV_OK;
 }
 
+int check_digests(const qkv_pages_t* p, const qkv_digests_t* d) {
+  if (!d || !d->layers || !d->exponents_dev) return QKV_ERR_NULL;
+  if (misaligned(d->exponents_dev, 16)) return QKV_ERR_ALIGN;
+  for (int i = 0; i < p->layers; ++i) {
+    if (!d->layers[i]) return QKV_ERR_NULL;
+    if (misaligned(d->layers[i], 16)) return QKV_ERR_ALIGN;
+  }
+  return QKV_OK;
+}
+
+uint32_t words_of(const qkv_pages_t* p) { return ((uint32_t)p->row_pages + 31u) / 32u; }
+
+// Scores in the workspace: of as many tiles of query tokens at a time as fit in kScoreBytes, or one.
+constexpr uint64_t kScoreBytes = 128ull << 20;
+struct ChoosePlan {
+  uint32_t per, stride, all, tiles;         // query tokens of a tile; scores of a (token, kv head); tiles in all and at a time
+  uint64_t bytes;
+};
+int plan_choose(const qkv_pages_t* p, int64_t tokens, uint32_t per, ChoosePlan& a) {
+  a.per = per;
+  a.stride = ((uint32_t)p->row_pages + 63u) / 64u * 64u;
+  a.all = per == 1u ? (uint32_t)p->rows : (uint32_t)(tokens / per) + (uint32_t)p->rows;
+  if ((uint64_t)a.all * (uint64_t)p->kv_heads >= (1ull << 23)) return QKV_ERR_SHAPE;
+  const uint64_t tile = (uint64_t)per * (uint64_t)p->kv_heads * a.stride * 4u;
+  // also few enough for a workgroup to each (token, kv head), of 1024 threads
+  const uint64_t fit = std::max<uint64_t>(1u, std::min<uint64_t>(kScoreBytes / tile, (1ull << 21) / ((uint64_t)per * (uint64_t)p->kv_heads)));
+  a.tiles = (uint32_t)std::min<uint64_t>(a.all, fit);
+  a.bytes = a.tiles * tile;
+  return QKV_OK;
+}
+int check_choose(const qkv_pages_t* p, int64_t tokens) {
+  if (tokens < 1 || tokens >= (1ll << 31) / 64 / p->kv_heads || p->row_pages >= (1 << 20)) return QKV_ERR_SHAPE;
+  return QKV_OK;
+}
+// Tiles of 64 tokens where there are enough of them that a digest is worth reading once for as many.
+uint32_t choose_per(const qkv_pages_t* p, int64_t tokens) { return tokens >= 64ll * p->rows && p->row_pages <= 16384 ? 64u : 16u; }
+
+struct ChosenPlan {
+  uint32_t rep, blocks, parts;
+  uint64_t floats, rows;                    // rows: of dimensions in the workspace
+};
+int plan_chosen(const qkv_pages_t* p, int32_t q_heads, int32_t most, ChosenPlan& a) {
+  if (most < 0) return QKV_ERR_SHAPE;
+  a.rep = (uint32_t)(q_heads / p->kv_heads);
+  a.blocks = (a.rep + 15u) / 16u;
+  const uint64_t items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
+  if (items >= (1ull << 22)) return QKV_ERR_SHAPE;
+  const uint64_t pages = most == 0 || most > p->row_pages ? (uint64_t)p->row_pages : (uint64_t)most;
+  const uint64_t turns = (pages * (uint64_t)p->page_tokens + kAttendTile * 4u - 1u) / (kAttendTile * 4u);      // of a workgroup's four waves
+  a.parts = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(items >= 512u ? 1u : 512u / items, turns));
+  a.rows = a.parts == 1u ? 0u : items * a.parts * std::min(16u, a.rep);
+  a.floats = a.rows * ((uint64_t)p->head_dim + 2u);
+  return QKV_OK;
+}
+
+// As for all pages, but that a workgroup's pairs share a list, and no part's length is known beforehand.
+int plan_prompt_chosen(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
+  if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
+  a.rep = (uint32_t)(q_heads / p->kv_heads);
+  a.waves = p->head_dim == 128 && tokens * q_heads >= kLargePrompt && p->page_tokens > 1 ? 8u : 4u;      // 64 keys of pages of one token are two words of a choice
+  a.per = 32u * a.waves / a.rep;
+  const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
+  if (tiles * a.waves * 64u >= (1ull << 32)) return QKV_ERR_SHAPE;
+  const uint64_t room = (uint64_t)p->row_pages * (uint64_t)p->page_tokens, groups = (uint64_t)((tokens + a.per - 1) / a.per) * (uint64_t)p->kv_heads;
+  a.least = 512u;
+  a.splits = a.waves == 8u || groups > 256u ? 1u : prompt_splits((uint32_t)std::min<uint64_t>(room, 1u << 30), groups > 8u ? (uint32_t)(512u / groups) : 64u);
+  a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
+  return QKV_OK;
+}
+int most_prompt_chosen_floats(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, uint64_t& floats) {
+  PromptPlan plan;
+  const int rc = plan_prompt_chosen(p, q_heads, tokens, plan);
+  if (rc) return rc;
+  floats = plan.floats;
+  // parts get fewer as query tiles get more: of the batches with as many tiles the one that fills them needs most, and behind 256 of them none has parts
+  const int64_t per = 128 / (int64_t)plan.rep;
+  for (int64_t n = per; n - per < tokens && (n / per - 1) * (int64_t)p->kv_heads <= 256; n += per) {
+    PromptPlan smaller;
+    if (plan_prompt_chosen(p, q_heads, std::min(n, tokens), smaller) == QKV_OK) floats = std::max(floats, smaller.floats);
+  }
+  return QKV_OK;
+}
+
+void set_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, const PromptPlan& plan, PagedPromptArgs& a) {
+  a.p = layer_of(pages, query->layer);
+  a.q = static_cast<const uint8_t*>(query->q_dev);
+  a.q_token_stride = (uint64_t)query->q_token_stride * 2u;
+  a.q_head_stride = (uint64_t)query->q_head_stride * 2u;
+  a.starts = query->starts_dev;
+  a.tokens = (uint32_t)query->tokens;
+  a.rep = plan.rep;
+  a.per = plan.per;
+  a.waves = plan.waves;
+  a.window = window_of(pages, query->window);
+  a.sinks = a.window ? (uint32_t)query->sinks : 0u;
+  a.scale_log2 = std::fabs(scale_of(query->softmax_scale));
+  a.flip = query->softmax_scale < 0.0f ? 1u : 0u;
+  a.out = static_cast<uint8_t*>(query->out_dev);
+  a.lse = query->lse_dev;
+  a.part_o = static_cast<float*>(query->workspace_dev);
+  a.part_ml = plan.floats ? a.part_o + plan.splits * (uint64_t)query->tokens * (uint64_t)query->q_heads * (uint64_t)pages->head_dim : nullptr;
+  a.splits = plan.splits;
+  a.least = plan.least;
+  a.status = query->status_dev;
+  a.choice = nullptr;
+  a.words = 0u;
+}
+
 }  // namespace
 
 extern "C" {
@@ -344,28 +452,207 @@ int qkv_paged_prompt(const qkv_pages_t* pages, const qkv_paged_query_t* query, v
   if (query->workspace_bytes < plan.floats * sizeof(float)) return QKV_ERR_CAPACITY;
   if (misaligned(query->workspace_dev, 16) || misaligned(query->starts_dev, 4)) return QKV_ERR_ALIGN;
   PagedPromptArgs a;
+  set_prompt(pages, query, plan, a);
+  return launch_paged_prompt(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_digest(const qkv_pages_t* pages, const qkv_digests_t* digests, const int32_t* starts_dev, int64_t tokens, int32_t layer_begin,
+                     int32_t layer_count, uint32_t* status_dev, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_digests(pages, digests);
+  if (rc) return rc;
+  if (layer_begin < 0 || layer_count < 1 || layer_begin > pages->layers - layer_count) return QKV_ERR_SHAPE;
+  if (tokens < 0 || tokens >= (1ll << 27) || (!starts_dev && tokens != pages->rows)) return QKV_ERR_SHAPE;
+  if ((uint64_t)(tokens / pages->page_tokens + pages->rows) * (uint64_t)pages->kv_heads >= (1ull << 24)) return QKV_ERR_SHAPE;      // 256 threads each, of a grid's 2^32
+  if (misaligned(starts_dev, 4) || misaligned(status_dev, 4)) return QKV_ERR_ALIGN;
+  DigestArgs a = {};
+  for (int i = 0; i < layer_count; ++i) {
+    a.k[i] = static_cast<const uint8_t*>(pages->k_layers[layer_begin + i]);
+    a.digest[i] = static_cast<int8_t*>(digests->layers[layer_begin + i]);
+  }
+  a.p = layer_of(pages, layer_begin);
+  a.exponents = digests->exponents_dev + (int64_t)layer_begin * pages->kv_heads * pages->head_dim;
+  a.starts = starts_dev;
+  a.tokens = (uint32_t)tokens;
+  a.layers = (uint32_t)layer_count;
+  a.status = status_dev;
+  return launch_pages_digest(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_paged_choose_workspace(const qkv_pages_t* pages, int64_t tokens, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_choose(pages, tokens);
+  if (rc) return rc;
+  uint64_t most = 0;
+  for (uint32_t per : {1u, 16u, 64u}) {                  // each needs no less for more tokens; which one it is hangs on their number
+    if (per == 64u && choose_per(pages, tokens) != 64u) continue;
+    if (per == 1u && tokens < pages->rows) continue;
+    ChoosePlan plan;
+    rc = plan_choose(pages, tokens, per, plan);
+    if (rc) return rc;
+    most = std::max(most, plan.bytes);
+  }
+  *bytes_out = most;
+  return QKV_OK;
+}
+
+int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, const qkv_choose_t* choose, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_digests(pages, digests);
+  if (rc) return rc;
+  if (!choose || !choose->q_dev || !choose->choice_dev) return QKV_ERR_NULL;
+  if (choose->layer < 0 || choose->layer >= pages->layers) return QKV_ERR_SHAPE;
+  rc = check_heads(pages, choose->q_heads);
+  if (rc) return rc;
+  if (choose->q_token_stride < 0 || choose->q_token_stride % 8 != 0 || choose->q_token_stride >= (1ll << 40) || choose->q_head_stride < 0 ||
+      choose->q_head_stride % 8 != 0 || choose->q_head_stride >= (1ll << 31))
+    return QKV_ERR_SHAPE;
+  if (choose->first < 0 || choose->last < 1 || (int64_t)choose->most < (int64_t)choose->first + choose->last) return QKV_ERR_SHAPE;
+  rc = check_choose(pages, choose->tokens);
+  if (rc) return rc;
+  if (!choose->starts_dev && choose->tokens != pages->rows) return QKV_ERR_SHAPE;
+  ChoosePlan plan;
+  rc = plan_choose(pages, choose->tokens, choose->starts_dev ? choose_per(pages, choose->tokens) : 1u, plan);
+  if (rc) return rc;
+  if (misaligned(choose->q_dev, 16) || misaligned(choose->choice_dev, 4) || misaligned(choose->starts_dev, 4) || misaligned(choose->status_dev, 4) ||
+      misaligned(choose->workspace_dev, 16))
+    return QKV_ERR_ALIGN;
+  if (plan.bytes != 0u && !choose->workspace_dev) return QKV_ERR_NULL;
+  if (choose->workspace_bytes < plan.bytes) return QKV_ERR_CAPACITY;
+  ChooseArgs a;
+  a.p = layer_of(pages, choose->layer);
+  a.q = static_cast<const uint8_t*>(choose->q_dev);
+  a.q_token_stride = (uint64_t)choose->q_token_stride * 2u;
+  a.q_head_stride = (uint64_t)choose->q_head_stride * 2u;
+  a.digest = static_cast<const int8_t*>(digests->layers[choose->layer]);
+  a.exponents = digests->exponents_dev + (int64_t)choose->layer * pages->kv_heads * pages->head_dim;
+  a.starts = choose->starts_dev;
+  a.tokens = (uint32_t)choose->tokens;
+  a.rep = (uint32_t)(choose->q_heads / pages->kv_heads);
+  a.per = plan.per;
+  a.first_tile = 0u;
+  a.tiles = plan.tiles;
+  a.most = (uint32_t)choose->most;
+  a.first = (uint32_t)choose->first;
+  a.last = (uint32_t)choose->last;
+  a.words = words_of(pages);
+  a.stride = plan.stride;
+  a.choice = choose->choice_dev;
+  a.status = choose->status_dev;
+  a.scores = static_cast<int32_t*>(choose->workspace_dev);
+  return launch_paged_choose(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_paged_attend_chosen_workspace(const qkv_pages_t* pages, int32_t q_heads, int32_t most, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_heads(pages, q_heads);
+  if (rc) return rc;
+  ChosenPlan plan;
+  rc = plan_chosen(pages, q_heads, most, plan);
+  if (rc) return rc;
+  *bytes_out = plan.floats * sizeof(float);
+  return QKV_OK;
+}
+
+int qkv_paged_attend_chosen(const qkv_pages_t* pages, const qkv_paged_query_t* query, const uint32_t* choice_dev, int32_t most, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!query || !choice_dev) return QKV_ERR_NULL;
+  rc = check_where(pages, query);
+  if (rc) return rc;
+  if (query->tokens != pages->rows || query->starts_dev || query->window != 0) return QKV_ERR_SHAPE;
+  if ((query->prior_out_dev == nullptr) != (query->prior_lse_dev == nullptr)) return QKV_ERR_NULL;
+  ChosenPlan plan;
+  rc = plan_chosen(pages, query->q_heads, most, plan);
+  if (rc) return rc;
+  if (plan.floats != 0u && !query->workspace_dev) return QKV_ERR_NULL;
+  if (query->workspace_bytes < plan.floats * sizeof(float)) return QKV_ERR_CAPACITY;
+  if (misaligned(query->workspace_dev, 16) || misaligned(query->prior_out_dev, 16) || misaligned(query->prior_lse_dev, 4) || misaligned(choice_dev, 4))
+    return QKV_ERR_ALIGN;
+  ChosenAttendArgs a;
   a.p = layer_of(pages, query->layer);
   a.q = static_cast<const uint8_t*>(query->q_dev);
   a.q_token_stride = (uint64_t)query->q_token_stride * 2u;
   a.q_head_stride = (uint64_t)query->q_head_stride * 2u;
-  a.starts = query->starts_dev;
-  a.tokens = (uint32_t)query->tokens;
+  a.choice = choice_dev;
+  a.words = words_of(pages);
   a.rep = plan.rep;
-  a.per = plan.per;
-  a.waves = plan.waves;
-  a.window = window_of(pages, query->window);
-  a.sinks = a.window ? (uint32_t)query->sinks : 0u;
-  a.scale_log2 = std::fabs(scale_of(query->softmax_scale));
-  a.flip = query->softmax_scale < 0.0f ? 1u : 0u;
-  a.out = static_cast<uint8_t*>(query->out_dev);
+  a.blocks = plan.blocks;
+  a.parts = plan.parts;
+  a.scale_log2 = scale_of(query->softmax_scale);
+  a.nothing = a.scale_log2 < 0.0f ? INFINITY : -INFINITY;
+  a.prior_out = query->prior_out_dev;
+  a.prior_lse = query->prior_lse_dev;
+  a.out = static_cast<float*>(query->out_dev);
   a.lse = query->lse_dev;
   a.part_o = static_cast<float*>(query->workspace_dev);
-  a.part_ml = plan.floats ? a.part_o + plan.splits * (uint64_t)query->tokens * (uint64_t)query->q_heads * (uint64_t)pages->head_dim : nullptr;
-  a.splits = plan.splits;
-  a.least = plan.least;
+  a.part_ml = plan.floats ? a.part_o + plan.rows * (uint64_t)pages->head_dim : nullptr;
   a.status = query->status_dev;
-  return launch_paged_prompt(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+  return launch_paged_attend_chosen(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_paged_prompt_chosen_workspace(const qkv_pages_t* pages, int32_t q_heads, int64_t tokens, uint64_t* bytes_out) {
+  if (!bytes_out) return QKV_ERR_NULL;
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  rc = check_heads(pages, q_heads);
+  if (rc) return rc;
+  uint64_t floats = 0;
+  rc = most_prompt_chosen_floats(pages, q_heads, tokens, floats);
+  if (rc) return rc;
+  *bytes_out = floats * sizeof(float);
+  return QKV_OK;
+}
+
+int qkv_paged_prompt_chosen(const qkv_pages_t* pages, const qkv_paged_query_t* query, const uint32_t* choice_dev, void* stream) {
+  int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!query || !query->starts_dev || !choice_dev) return QKV_ERR_NULL;
+  rc = check_where(pages, query);
+  if (rc) return rc;
+  if (query->prior_out_dev || query->prior_lse_dev || query->window != 0) return QKV_ERR_SHAPE;
+  PromptPlan plan;
+  rc = plan_prompt_chosen(pages, query->q_heads, query->tokens, plan);
+  if (rc) return rc;
+  if (plan.floats != 0u && !query->workspace_dev) return QKV_ERR_NULL;
+  if (query->workspace_bytes < plan.floats * sizeof(float)) return QKV_ERR_CAPACITY;
+  if (misaligned(query->workspace_dev, 16) || misaligned(query->starts_dev, 4) || misaligned(choice_dev, 4)) return QKV_ERR_ALIGN;
+  PagedPromptArgs a;
+  set_prompt(pages, query, plan, a);
+  a.choice = choice_dev;
+  a.words = words_of(pages);
+  return launch_paged_prompt_chosen(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? QKV_OK : QKV_ERR_HIP;
+}
+
+int qkv_pages_slots(const qkv_pages_t* pages, const qkv_slots_t* slots, uint32_t* status_dev, void* stream) {
+  const int rc = check_pages(pages, false);
+  if (rc) return rc;
+  if (!slots || !slots->starts_dev) return QKV_ERR_NULL;
+  if (slots->tokens < 1 || slots->tokens >= (1ll << 27)) return QKV_ERR_SHAPE;
+  if (misaligned(slots->more_dev, 4) || misaligned(slots->starts_dev, 4) || misaligned(slots->row_dev, 4) || misaligned(slots->place_dev, 4) ||
+      misaligned(slots->slot_dev, 8) || misaligned(status_dev, 4))
+    return QKV_ERR_ALIGN;
+  SlotsArgs a;
+  a.p = layer_of(pages, 0);
+  a.more = slots->more_dev;
+  a.tokens = (uint32_t)slots->tokens;
+  a.starts = slots->starts_dev;
+  a.row = slots->row_dev;
+  a.place = slots->place_dev;
+  a.slot = slots->slot_dev;
+  a.status = status_dev;
+  return launch_pages_slots(a, static_cast<hipStream_t>(stream)) == hipSuccess ? QKV_OK : QKV_ERR_HIP;
 }
 
 }  // extern "C"
