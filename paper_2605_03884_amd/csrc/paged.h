@@ -219,7 +219,7 @@ struct ChooseArgs {
   uint32_t most, first, last;
   uint32_t words, stride;                                // of a choice; scores of a (token, kv head) in the workspace
   uint32_t *choice, *status;
-  int32_t* scores;                                       // [tiles][per][kv heads][stride]
+  int32_t* scores;                                       // [tiles][per][kv heads][stride]; null where they stay in LDS
 };
 
 struct ChosenAttendArgs {

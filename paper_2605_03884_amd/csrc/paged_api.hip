@@ -198,30 +198,52 @@ int check_digests(const qkv_pages_t* p, const qkv_digests_t* d) {
 
 uint32_t words_of(const qkv_pages_t* p) { return ((uint32_t)p->row_pages + 31u) / 32u; }
 
-// Scores in the workspace: of as many tiles of query tokens at a time as fit in kScoreBytes, or one.
+// Scores stay in LDS where they fit, and there are enough tiles or few pages to each; otherwise they go through the workspace, those of as many tiles of query
+// tokens at a time as fit in kScoreBytes, or of one.
 constexpr uint64_t kScoreBytes = 128ull << 20;
 struct ChoosePlan {
   uint32_t per, stride, all, tiles;         // query tokens of a tile; scores of a (token, kv head); tiles in all and at a time
   uint64_t bytes;
 };
-int plan_choose(const qkv_pages_t* p, int64_t tokens, uint32_t per, ChoosePlan& a) {
-  a.per = per;
+int plan_choose(const qkv_pages_t* p, int64_t tokens, bool single, ChoosePlan& a) {
   a.stride = ((uint32_t)p->row_pages + 63u) / 64u * 64u;
-  a.all = per == 1u ? (uint32_t)p->rows : (uint32_t)(tokens / per) + (uint32_t)p->rows;
-  if ((uint64_t)a.all * (uint64_t)p->kv_heads >= (1ull << 23)) return QKV_ERR_SHAPE;
-  const uint64_t tile = (uint64_t)per * (uint64_t)p->kv_heads * a.stride * 4u;
+  const uint64_t items = (uint64_t)p->rows * (uint64_t)p->kv_heads;
+  const bool enough = tokens >= 32ll * p->rows, within = single ? a.stride <= 1024u || (a.stride <= 2048u && items >= 256u) : a.stride <= 768u;
+  a.per = single ? 1u : !within ? (enough && a.stride <= 16384u ? 64u : 16u) : enough && a.stride <= 384u ? 32u : 16u;
+  a.all = single ? (uint32_t)p->rows : (uint32_t)(tokens / a.per) + (uint32_t)p->rows;
+  if ((uint64_t)a.all * (uint64_t)p->kv_heads >= (1ull << 23)) return QKV_ERR_SHAPE;     // 512 threads each, of a grid's 2^32
+  a.tiles = a.all;
+  a.bytes = 0u;
+  if (within) return QKV_OK;
+  const uint64_t tile = (uint64_t)a.per * (uint64_t)p->kv_heads * a.stride * 4u;
   // also few enough for a workgroup to each (token, kv head), of 1024 threads
-  const uint64_t fit = std::max<uint64_t>(1u, std::min<uint64_t>(kScoreBytes / tile, (1ull << 21) / ((uint64_t)per * (uint64_t)p->kv_heads)));
+  const uint64_t fit = std::max<uint64_t>(1u, std::min<uint64_t>(kScoreBytes / tile, (1ull << 21) / ((uint64_t)a.per * (uint64_t)p->kv_heads)));
   a.tiles = (uint32_t)std::min<uint64_t>(a.all, fit);
   a.bytes = a.tiles * tile;
+  return QKV_OK;
+}
+// What is enough for every batch of up to `tokens`: tiles get larger with their number, and the largest that are cut off at kScoreBytes need not be those of most tokens.
+int most_choose_bytes(const qkv_pages_t* p, int64_t tokens, uint64_t& bytes) {
+  bytes = 0u;
+  const int64_t border = 32ll * p->rows - 1;
+  for (int64_t n : {tokens, std::min(tokens, border)}) {
+    ChoosePlan plan;
+    const int rc = plan_choose(p, n, false, plan);
+    if (rc) return rc;
+    bytes = std::max(bytes, plan.bytes);
+  }
+  if (tokens >= p->rows) {
+    ChoosePlan plan;
+    const int rc = plan_choose(p, p->rows, true, plan);
+    if (rc) return rc;
+    bytes = std::max(bytes, plan.bytes);
+  }
   return QKV_OK;
 }
 int check_choose(const qkv_pages_t* p, int64_t tokens) {
   if (tokens < 1 || tokens >= (1ll << 31) / 64 / p->kv_heads || p->row_pages >= (1 << 20)) return QKV_ERR_SHAPE;
   return QKV_OK;
 }
-// Tiles of 64 tokens where there are enough of them that a digest is worth reading once for as many.
-uint32_t choose_per(const qkv_pages_t* p, int64_t tokens) { return tokens >= 64ll * p->rows && p->row_pages <= 16384 ? 64u : 16u; }
 
 struct ChosenPlan {
   uint32_t rep, blocks, parts;
@@ -488,17 +510,7 @@ int qkv_paged_choose_workspace(const qkv_pages_t* pages, int64_t tokens, uint64_
   if (rc) return rc;
   rc = check_choose(pages, tokens);
   if (rc) return rc;
-  uint64_t most = 0;
-  for (uint32_t per : {1u, 16u, 64u}) {                  // each needs no less for more tokens; which one it is hangs on their number
-    if (per == 64u && choose_per(pages, tokens) != 64u) continue;
-    if (per == 1u && tokens < pages->rows) continue;
-    ChoosePlan plan;
-    rc = plan_choose(pages, tokens, per, plan);
-    if (rc) return rc;
-    most = std::max(most, plan.bytes);
-  }
-  *bytes_out = most;
-  return QKV_OK;
+  return most_choose_bytes(pages, tokens, *bytes_out);
 }
 
 int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, const qkv_choose_t* choose, void* stream) {
@@ -518,7 +530,7 @@ int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, con
   if (rc) return rc;
   if (!choose->starts_dev && choose->tokens != pages->rows) return QKV_ERR_SHAPE;
   ChoosePlan plan;
-  rc = plan_choose(pages, choose->tokens, choose->starts_dev ? choose_per(pages, choose->tokens) : 1u, plan);
+  rc = plan_choose(pages, choose->tokens, !choose->starts_dev, plan);
   if (rc) return rc;
   if (misaligned(choose->q_dev, 16) || misaligned(choose->choice_dev, 4) || misaligned(choose->starts_dev, 4) || misaligned(choose->status_dev, 4) ||
       misaligned(choose->workspace_dev, 16))
@@ -545,7 +557,7 @@ int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, con
   a.stride = plan.stride;
   a.choice = choose->choice_dev;
   a.status = choose->status_dev;
-  a.scores = static_cast<int32_t*>(choose->workspace_dev);
+  a.scores = plan.bytes ? static_cast<int32_t*>(choose->workspace_dev) : nullptr;
   return launch_paged_choose(a, (uint32_t)pages->head_dim, pages->value_type == QKV_VALUE_BF16, static_cast<hipStream_t>(stream)) == hipSuccess
              ? QKV_OK : QKV_ERR_HIP;
 }

@@ -59,7 +59,7 @@ __device__ inline FilledPage filled_page(const DigestArgs& a, uint32_t at, uint3
 // A wave takes a (page, kv head), or all waves of a workgroup do: D / 8 lanes read a row, 64 / (D / 8) rows at once.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(kDigestThreads) void digest_kernel(DigestArgs a) {
-  constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes, kAtOnce = 4;
+  constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes, kAtOnce = 8;
   constexpr short kInfinity = (short)T::kExponent;
   __shared__ i16x8 parts[SPLIT ? kDigestWaves : 1u][2][kRowLanes];
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kDigestThreads) void digest_kernel(DigestArgs a) {
     i16x8 x[kAtOnce];
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j)               // behind the page's end its first row of the loop again
-      x[j] = __builtin_bit_cast(i16x8, *reinterpret_cast<const u32x4*>(keys + (uint64_t)(t + j * kRowsAtOnce < size ? t + j * kRowsAtOnce : t) * a.p.token_stride));
+      x[j] = __builtin_bit_cast(i16x8, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(keys + (uint64_t)(t + j * kRowsAtOnce < size ? t + j * kRowsAtOnce : t) * a.p.token_stride)));
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j) {
       const i16x8 y = ordered(x[j]);
