@@ -267,13 +267,13 @@ int plan_chosen(const qkv_pages_t* p, int32_t q_heads, int32_t most, ChosenPlan&
 int plan_prompt_chosen(const qkv_pages_t* p, int32_t q_heads, int64_t tokens, PromptPlan& a) {
   if (tokens < 1 || tokens >= (1ll << 31) / q_heads) return QKV_ERR_SHAPE;
   a.rep = (uint32_t)(q_heads / p->kv_heads);
-  a.waves = p->head_dim == 128 && tokens * q_heads >= kLargePrompt && p->page_tokens > 1 ? 8u : 4u;      // 64 keys of pages of one token are two words of a choice
+  a.waves = 4u;
   a.per = 32u * a.waves / a.rep;
   const uint64_t tiles = (uint64_t)(tokens / a.per + p->rows) * (uint64_t)p->kv_heads;
   if (tiles * a.waves * 64u >= (1ull << 32)) return QKV_ERR_SHAPE;
   const uint64_t room = (uint64_t)p->row_pages * (uint64_t)p->page_tokens, groups = (uint64_t)((tokens + a.per - 1) / a.per) * (uint64_t)p->kv_heads;
   a.least = 512u;
-  a.splits = a.waves == 8u || groups > 256u ? 1u : prompt_splits((uint32_t)std::min<uint64_t>(room, 1u << 30), groups > 8u ? (uint32_t)(512u / groups) : 64u);
+  a.splits = groups > 256u ? 1u : prompt_splits((uint32_t)std::min<uint64_t>(room, 1u << 30), groups > 8u ? (uint32_t)(512u / groups) : 64u);
   a.floats = a.splits == 1u ? 0u : a.splits * (uint64_t)tokens * (uint64_t)q_heads * ((uint64_t)p->head_dim + 2u);
   return QKV_OK;
 }
