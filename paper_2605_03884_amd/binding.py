@@ -805,16 +805,14 @@ def paged_prompt_chosen(pages, choice, q, starts, softmax_scale, out, lse=None, 
 def pages_slots(pages, starts, row=None, place=None, slot=None, more=None, tokens=None, status=None, stream=None):
     """The maps of a ragged batch from how many new tokens each row has (more: device int32 [rows]; None: one for every row that has any).  Written: starts, device
     int32 [rows + 1]; row and place, device int32 [tokens], and slot, int64 [tokens], those that are given (without any, tokens is the room a batch has)."""
-    given = [t for t in (row, place, slot) if t is not None]
-    if given:
-        if tokens is not None and tokens != given[0].numel():
-            raise ValueError("the maps must have room for the batch's tokens")
-        tokens = given[0].numel()
-    elif tokens is None:
+    some = row if row is not None else place if place is not None else slot
+    if some is None and tokens is None:
         raise ValueError("without a map the room for tokens has to be given")
-    x = Slots(0 if more is None else _of_pages(more, pages, torch.int32, (pages.rows,), "more"), tokens,
-              _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts"))
-    for name, t, kind in (("row", row, torch.int32), ("place", place, torch.int32), ("slot", slot, torch.int64)):
-        if t is not None:
-            setattr(x, name + "_dev", _of_pages(t, pages, kind, (tokens,), name))
+    n = tokens if some is None else some.numel()
+    if tokens is not None and tokens != n:
+        raise ValueError("the maps must have room for the batch's tokens")
+    wide = (n,)
+    x = Slots(0 if more is None else _of_pages(more, pages, torch.int32, (pages.rows,), "more"), n, _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts"),
+              0 if row is None else _of_pages(row, pages, torch.int32, wide, "row"), 0 if place is None else _of_pages(place, pages, torch.int32, wide, "place"),
+              0 if slot is None else _of_pages(slot, pages, torch.int64, wide, "slot"))
     _check(lib().qkv_pages_slots(pages, x, _status_of_pages(status, pages), _here(pages, stream)), "qkv_pages_slots")

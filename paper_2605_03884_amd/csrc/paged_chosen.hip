@@ -22,6 +22,7 @@ constexpr uint32_t kChosenThreads = 256, kChosenWaves = kChosenThreads / kWaveSi
 constexpr uint32_t kChosenWords = kChosenThreads;        // words of a choice that are turned into a list at a time
 constexpr uint32_t kChosenPages = kChosenWords * 32u;
 constexpr uint32_t kNoPage = 0xFFFFFFFFu;
+constexpr uint32_t kChosenTable = 2048;                  // entries of a row, up to which they are read beside lengths and bits: one trip to memory less in front of the keys
 
 // RUN: tokens of a tile that surely lie in one page: 32, or 1 where pages are smaller.
 template <typename T, int D, uint32_t RUN>
@@ -31,7 +32,8 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
   constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes;
   __shared__ __attribute__((aligned(256))) uint8_t lds[kChosenWaves][kAttendTile * D * 2];      // values, then the waves' sums: 16 heads of D floats
   static_assert(kAttendTile * D * 2 == 16 * D * 4);
-  __shared__ uint32_t list[kChosenPages];
+  __shared__ uint32_t list[kChosenPages];                              // and behind kChosenTable of them a row's entries, where it has no more
+  static_assert(kChosenPages >= 2u * kChosenTable);
   __shared__ f32x2 tops[kChosenWaves][16];
   __shared__ uint32_t counts[2][kChosenWaves];
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
@@ -47,11 +49,22 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
   const uint8_t* keys = a.p.k + (uint64_t)head * a.p.head_stride;
   const uint8_t* values = a.p.v + (uint64_t)head * a.p.head_stride;
   uint8_t* mine = lds[wave];
-  const auto word_at = [&](uint32_t w) -> uint32_t {                   // bits of pages that are in sight
-    if (w * 32u >= all) return 0u;
-    const uint32_t x = bits[w], rest = all - w * 32u;
+  const auto in_sight = [&](uint32_t w, uint32_t x) -> uint32_t {      // of a word, the bits of pages that are in sight
+    const uint32_t rest = all > w * 32u ? all - w * 32u : 0u;
     return rest < 32u ? x & ((1u << rest) - 1u) : x;
   };
+  const auto word_at = [&](uint32_t w) -> uint32_t { return w * 32u < all ? in_sight(w, bits[w]) : 0u; };
+  const bool staged = a.p.row_pages <= kChosenTable;
+  const uint32_t first_bits = threadIdx.x < a.words ? bits[threadIdx.x] : 0u;
+  if (staged) {
+    uint32_t x[kChosenTable / kChosenThreads];
+#pragma unroll
+    for (uint32_t i = 0; i < kChosenTable / kChosenThreads; ++i)
+      if (i * kChosenThreads < a.p.row_pages) x[i] = (uint32_t)entries[min(i * kChosenThreads + threadIdx.x, a.p.row_pages - 1u)];
+#pragma unroll
+    for (uint32_t i = 0; i < kChosenTable / kChosenThreads; ++i)
+      if (i * kChosenThreads < a.p.row_pages) list[kChosenTable + i * kChosenThreads + threadIdx.x] = x[i];
+  }
   typename T::x8 q[kSteps];
 #pragma unroll
   for (uint32_t k = 0; k < kSteps; ++k) {
@@ -67,7 +80,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
   uint32_t turn = 0u;
   for (uint32_t first_word = 0; first_word * 32u < all; first_word += kChosenWords) {
     // the list of this stretch's pages, in their order
-    uint32_t word = word_at(first_word + threadIdx.x);
+    uint32_t word = first_word == 0u ? in_sight(threadIdx.x, first_bits) : word_at(first_word + threadIdx.x);
     const uint32_t upto = wave_inclusive_scan((uint32_t)__builtin_popcount(word));
     if (lane == kWaveSize - 1u) counts[turn][wave] = upto;
     __syncthreads();                                                   // nobody is at the last stretch's list any more
@@ -87,7 +100,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
     const bool own = total != 0u && list[total - 1u] == all - 1u;      // the page that need not be full is the last one
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < total; i += kChosenThreads) {
-      const uint32_t page = (uint32_t)entries[list[i]];
+      const uint32_t page = staged ? list[kChosenTable + list[i]] : (uint32_t)entries[list[i]];
       list[i] = page < a.p.pages ? page : kNoPage;
       if (page >= a.p.pages) flag(a.status, QKV_STATUS_BAD_PAGE);
     }

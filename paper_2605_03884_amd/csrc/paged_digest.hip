@@ -59,7 +59,7 @@ __device__ inline FilledPage filled_page(const DigestArgs& a, uint32_t at, uint3
 // A wave takes a (page, kv head), or all waves of a workgroup do: D / 8 lanes read a row, 64 / (D / 8) rows at once.
 template <typename T, int D, bool SPLIT>
 __global__ __launch_bounds__(kDigestThreads) void digest_kernel(DigestArgs a) {
-  constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes, kAtOnce = 8;
+  constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes, kAtOnce = 4;
   constexpr short kInfinity = (short)T::kExponent;
   __shared__ i16x8 parts[SPLIT ? kDigestWaves : 1u][2][kRowLanes];
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
