@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
   };
   const auto first_key = [](int32_t half) { return half & ~1; };
   // Whether all pairs whose first query stands at `place` see all of a half.
-  const auto whole = [&](int32_t half, int32_t place) { return (half & 1) != 0 && first_key(half) + 32 <= place + 1; };
+  const auto whole = [&](int32_t half, int32_t place) { return (half & 1) != 0 && first_key(half) <= place - 31; };
   const auto make_list = [&]() {
     const uint32_t count = min(kListWords, (in_sight + 31u) / 32u - first_word);
     __syncthreads();                                                   // nobody is at the last stretch's list any more
@@ -253,7 +253,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
   };
   const auto store_values = [&](const Tile& t, uint32_t place) {
     // Rows that nobody sees may hold anything: behind the sequence nothing has been written yet.
-    const bool cut = first_key(t.half[1]) + 32 > reach || (RUN != 64u && span_pages != 1u);
+    const bool cut = first_key(t.half[1]) > reach - 32 || (RUN != 64u && span_pages != 1u);
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
       if (cut && !seen_by_some(key_of(t, j * kRowsAtOnce + my_row))) vx[j] = (u32x4)(0u);
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
     const int32_t t = first_key(tile.half[half]);
     if constexpr (RUN != 1u) {
       // all in front of the wave's first query: 16 keys at least are one page's, and a bit that is the same for all of them is a mask of lanes
-      if (special == 0u && t + 31 <= wave_first) {
+      if (special == 0u && t <= wave_first - 31) {
         const bool one = word >> ((uint32_t)t >> page_shift) % 32u & 1u, two = RUN == 64u ? one : word >> ((uint32_t)(t + 16) >> page_shift) % 32u & 1u;
         if (__builtin_amdgcn_ballot_w64(!one || !two) == 0ull) return;
 #pragma unroll
