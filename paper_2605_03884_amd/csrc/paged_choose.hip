@@ -145,7 +145,7 @@ __device__ inline void query_codes(const ChooseArgs& a, const QueryTile& t, uint
 template <int D, uint32_t GROUPS, uint32_t WAVES, typename Prepare, typename Put>
 __device__ inline void score_pages(const ChooseArgs& a, const QueryTile& t, uint32_t head, uint32_t lane, uint32_t wave, const int8_t* codes, uint32_t begin, uint32_t end,
                                    Prepare prepare, Put put) {
-  constexpr uint32_t kSteps = 2u * D / 64u, kTurns = D == 256 ? 2u : 4u;      // 16 pages in flight, of four: as many as there are registers for
+  constexpr uint32_t kSteps = 2u * D / 64u, kTurns = 2u;      // of 16 pages, in flight at a time
   const uint32_t n = lane % 16u, g = lane / 16u;
   const int32_t* entries = a.p.table + (uint64_t)t.row * a.p.row_pages;
   const int8_t* digests = a.digest + (uint64_t)head * (2u * D) + g * 16u;
@@ -444,16 +444,19 @@ hipError_t launch_choose_of(const ChooseArgs& given, hipStream_t stream) {
   const uint32_t all = a.starts ? places(a.tokens, a.p.rows, a.per) : a.p.rows, at_once = a.tiles;
   for (a.first_tile = 0u; a.first_tile < all; a.first_tile += at_once) {
     a.tiles = std::min(at_once, all - a.first_tile);
-    // Few tiles: their pages in stretches, until there are two workgroups to a CU, of 64 pages at least.
+    // Few tiles: their pages in stretches, until there are four workgroups to a CU, of 64 pages at least (131071 tokens in pages of 16, 8 kv heads: 4.8 us, with two 5.7).
     const uint32_t groups = a.tiles * a.p.kv_heads, pages = (a.p.row_pages + 63u) / 64u;
-    const uint32_t cuts = std::min(pages, groups >= 512u ? 1u : (511u + groups) / groups), chunk = (pages + cuts - 1u) / cuts * 64u;
+    const uint32_t cuts = std::min(pages, groups >= 1024u ? 1u : (1023u + groups) / groups), chunk = (pages + cuts - 1u) / cuts * 64u;
     const dim3 grid(groups, (a.p.row_pages + chunk - 1u) / chunk);
     if (!a.starts || a.per == 16u) score_kernel<T, D, 1u><<<grid, kScoreThreads, 0, stream>>>(a, chunk);
     else score_kernel<T, D, 4u><<<grid, kScoreThreads, 0, stream>>>(a, chunk);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t units = a.tiles * a.per * a.p.kv_heads;
-    if (a.stride <= kPickWaves * 64u * 16u) choose_kernel<16u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
+    // blocks of 64 pages a wave keeps: those it has not are looked at too (8193 pages: 5.9 us with 9, 7.6 with 16)
+    if (a.stride <= kPickWaves * 64u * 4u) choose_kernel<4u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
+    else if (a.stride <= kPickWaves * 64u * 9u) choose_kernel<9u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
+    else if (a.stride <= kPickWaves * 64u * 16u) choose_kernel<16u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
     else choose_kernel<0u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;

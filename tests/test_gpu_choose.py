@@ -86,7 +86,7 @@ def test_prompts(kind, dim):
     assert int(x.cache.status) == 0
 
 
-@pytest.mark.parametrize("pages", [1023, 1025, 1100, 2049])
+@pytest.mark.parametrize("pages", [1023, 1025, 1100, 2049, 5000, 12000])
 def test_many_pages(pages):
     x = Scored([pages, pages - 1, 5], 1, 2, 64, 1, seed=pages)
     x.check(100, 3, 4)
