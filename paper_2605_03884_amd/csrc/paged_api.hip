@@ -198,8 +198,12 @@ int check_digests(const qkv_pages_t* p, const qkv_digests_t* d) {
 
 uint32_t words_of(const qkv_pages_t* p) { return ((uint32_t)p->row_pages + 31u) / 32u; }
 
-// Scores stay in LDS where they fit, and there are enough tiles or few pages to each; otherwise they go through the workspace, those of as many tiles of query
-// tokens at a time as fit in kScoreBytes, or of one.
+// Scores stay in LDS where they fit and there are enough tiles or few pages to each; otherwise they go through the workspace, those of as many tiles of query tokens at a
+// time as fit in kScoreBytes, or of one.  In us, 8 kv heads of 128 dimensions:
+//   one token of a row       1 row of 300 pages 7.4 in LDS, 8.2 through the workspace; of 1000 pages 12.3, 8.6; 16 rows of 1000 pages 12.3, 12.0; 32 rows 13.9, 16.4; 64 rows of 2040 pages 33, 37
+//   16 tokens a tile in LDS  with more than 768 pages a workgroup fills a CU: 600 tokens of 1000 pages 17.2, 28.2; of 1500 22.9, 33.8; 3000 tokens of 1000 pages 80, 63
+//   32 tokens a tile in LDS  3000 tokens of 180 pages 25, in tiles of 16 34; 1200 tokens 12.9, 12.9; 600 tokens 13.1, 11.3
+//   64 through the workspace 512 tokens of 2 heads and 12000 pages 53.7, in tiles of 16 59.7; of 20000 pages 119, 129
 constexpr uint64_t kScoreBytes = 128ull << 20;
 struct ChoosePlan {
   uint32_t per, stride, all, tiles;         // query tokens of a tile; scores of a (token, kv head); tiles in all and at a time
@@ -208,8 +212,10 @@ struct ChoosePlan {
 int plan_choose(const qkv_pages_t* p, int64_t tokens, bool single, ChoosePlan& a) {
   a.stride = ((uint32_t)p->row_pages + 63u) / 64u * 64u;
   const uint64_t items = (uint64_t)p->rows * (uint64_t)p->kv_heads;
-  const bool enough = tokens >= 32ll * p->rows, within = single ? a.stride <= 1024u || (a.stride <= 2048u && items >= 256u) : a.stride <= 768u;
-  a.per = single ? 1u : !within ? (enough && a.stride <= 16384u ? 64u : 16u) : enough && a.stride <= 384u ? 32u : 16u;
+  const bool enough = tokens >= 32ll * p->rows;
+  const uint64_t tiles_of_16 = ((uint64_t)tokens / 16u + (uint64_t)p->rows) * (uint64_t)p->kv_heads;
+  const bool within = single ? a.stride <= 512u || (a.stride <= 2048u && items >= 256u) : a.stride <= 768u || (a.stride <= 1536u && tiles_of_16 <= 768u);
+  a.per = single ? 1u : !within ? (enough && 64u * (uint64_t)p->kv_heads * a.stride * 4u <= kScoreBytes ? 64u : 16u) : enough && a.stride <= 384u && (uint64_t)tokens * (uint64_t)p->kv_heads >= 8192u ? 32u : 16u;
   a.all = single ? (uint32_t)p->rows : (uint32_t)(tokens / a.per) + (uint32_t)p->rows;
   if ((uint64_t)a.all * (uint64_t)p->kv_heads >= (1ull << 23)) return QKV_ERR_SHAPE;     // 512 threads each, of a grid's 2^32
   a.tiles = a.all;
@@ -255,6 +261,7 @@ int plan_chosen(const qkv_pages_t* p, int32_t q_heads, int32_t most, ChosenPlan&
   a.blocks = (a.rep + 15u) / 16u;
   const uint64_t items = (uint64_t)p->rows * (uint64_t)p->kv_heads * a.blocks;
   if (items >= (1ull << 22)) return QKV_ERR_SHAPE;
+  // Few items: parts, until there are two workgroups to a CU.  16 rows of 8 kv heads, 64 pages of 16: 19.9 us, with one to a CU 20.3, with four 23.7; 8 rows, 256 pages: 29.2, 30.6, 33.3.
   const uint64_t pages = most == 0 || most > p->row_pages ? (uint64_t)p->row_pages : (uint64_t)most;
   const uint64_t turns = (pages * (uint64_t)p->page_tokens + kAttendTile * 4u - 1u) / (kAttendTile * 4u);      // of a workgroup's four waves
   a.parts = (uint32_t)std::max<uint64_t>(1u, std::min<uint64_t>(items >= 512u ? 1u : 512u / items, turns));

@@ -6,9 +6,16 @@
 // A score is a product of two rows of 2 D codes, so the scores of 16 pages with 16 tokens are one chain of v_mfma_i32_16x16x64_i8, which reads the digests as they lie
 // in memory.  It is below 2^23 (127 * 128 * 2 * 256) and exact.
 //
-// First kernel: a workgroup takes a tile of query tokens of one kv head and a stretch of pages, works the tokens' codes out into LDS and goes through the pages, 16 a
-// wave.  Second kernel: a token and kv head is a wave's or a workgroup's; its scores stay in registers while bisection finds the score of the last page
-// that is chosen, and a ballot writes 64 bits of the choice at once.
+// Where scores fit LDS one kernel does: a workgroup takes one token, or a tile of 16 or 32 tokens of one sequence, with a kv head.  Its waves work the tokens' codes
+// out into LDS, go through the pages in sight, 64 a wave at a time with the digests of 32 on their way, and put the scores into LDS.  Then a token is a wave's, or the one token
+// all waves': its scores stay in registers while counting finds the last one that is chosen, and a ballot writes 64 bits of the choice at once.  Otherwise one kernel
+// writes the scores of stretches of pages to the workspace and a second one picks.
+//
+// What bounds it: many tokens, instructions.  6583 tokens of two prompts behind up to 8000, pages of 32, 8 kv heads of 128 dimensions: 54.6 us for 58 MB (12 us of a copy) and 7.4 G
+// operations; vector instructions issue in 54 % of the cycles, 373 for each of 52664 choices.  Single tokens, one chain: lengths, entries, digests, scores, picks.  48 rows of up to 8192
+// tokens in pages of 16: 11.6 us for 26 MB; 131071 tokens of one row: 13.3 us for 16.8 MB, 6.2 for the scores and 7 for the picks, which are those of 8 workgroups.
+// What steps were worth, these three: scores in LDS and counting (8 bits a look) in place of bisection over the workspace (a bit a look) 128.6 -> 59, 19.5 -> 12.8 and 22.4 -> 14.6 us; of it no
+// branches in a wave's blocks 70 -> 57 (with 16 tokens a tile 71 where 32 have 57).  A wave or two for each of many choices, in place of 16 that wait for each other: 3000 tokens of 4000 pages 347 -> 202.
 #include <algorithm>
 
 #include "paged.h"
@@ -213,12 +220,14 @@ __device__ inline void score_pages(const ChooseArgs& a, const QueryTile& t, uint
 // The last score that is chosen is found by counting: how far scores lie below the highest one, in 256 steps that are powers of two, then the step in which the place
 // `most` falls in 256 steps of its own, until all of a step are chosen or the step is a single score.  At most 3 rounds, mostly 1 or 2.  What a wave does with a block
 // is written without branches: a wave that has few of them spends its time on issuing instructions.
+constexpr uint32_t kOutOfRange = 16;                     // places for what is out of range, so that lanes do not wait for each other at one
+template <uint32_t WAVES>
 struct PickSpace {
-  uint32_t counts[256 + kWaveSize];                      // and where what is out of range goes, lanes apart
-  int32_t shared[2][16];
+  uint32_t counts[256 + kOutOfRange];
+  int32_t shared[2][WAVES];
 };
 template <uint32_t WAVES, uint32_t KEEP, bool CHEAP, typename Without>
-__device__ inline void pick(const ChooseArgs& a, uint32_t lane, uint32_t wave, uint32_t all, PickSpace& space, const int32_t* scores, uint32_t* choice, Without without) {
+__device__ inline void pick(const ChooseArgs& a, uint32_t lane, uint32_t wave, uint32_t all, PickSpace<WAVES>& space, const int32_t* scores, uint32_t* choice, Without without) {
   const uint32_t scored = all > a.last ? all - a.last : 0u, span = scored > a.first ? scored - a.first : 0u;       // pages with scores: `first` and on
   const uint32_t blocks = (all + 63u) / 64u, each = (blocks + WAVES - 1u) / WAVES, from = min(wave * each, blocks), upto = min(from + each, blocks);
   const uint32_t last_block = max(blocks, 1u) - 1u, end = min(all, upto * 64u);
@@ -280,7 +289,7 @@ __device__ inline void pick(const ChooseArgs& a, uint32_t lane, uint32_t wave, u
       for (uint32_t i = 0; from + i < upto; ++i) look(i, settled(from + i, scores[(from + i) * 64u + lane]));
     }
   };
-  uint32_t left = a.most - 1u, shift = min(16u, (uint32_t)max(0, 24 - (int)__builtin_clz((uint32_t)(top - low) | 1u)));
+  uint32_t left = a.most - 1u, shift = min(16u, (uint32_t)max(0, 24 - (int)__builtin_clz(((uint32_t)top - (uint32_t)low) | 1u)));
   int32_t least;                                                       // chosen: what is above, and ...
   uint32_t equal = 0xFFFFFFFFu;                                        // ... so many of those that are equal, from the front; all of them by default
   const int32_t highest = top;
@@ -289,7 +298,7 @@ __device__ inline void pick(const ChooseArgs& a, uint32_t lane, uint32_t wave, u
     sync();
     each_block([&](uint32_t, int32_t x) {
       const uint32_t step = ((uint32_t)top - (uint32_t)min(x, highest)) >> shift;      // what is out of range either way is beyond 255
-      atomicAdd(&space.counts[min(step, 256u + lane)], 1u);
+      atomicAdd(&space.counts[min(step, 256u + lane % kOutOfRange)], 1u);
     });
     sync();
     // lane l: the steps 4 l .. 4 l + 3
@@ -362,12 +371,12 @@ __device__ inline void pick(const ChooseArgs& a, uint32_t lane, uint32_t wave, u
 __device__ inline uint32_t in_sight(const ChooseArgs& a, int32_t place) { return place < 0 ? 0u : ((uint32_t)place >> a.p.page_shift) + 1u; }
 
 // One kernel for a tile of up to 16 GROUPS tokens of a kv head, where their scores fit LDS: tokens are taken by a wave each, or (ONE: a tile is one token) by all.
-constexpr uint32_t kTileThreads = 512, kTileWaves = kTileThreads / kWaveSize;
-template <typename T, int D, uint32_t GROUPS, uint32_t KEEP, bool ONE>
-__global__ __launch_bounds__(kTileThreads) void choose_tile_kernel(ChooseArgs a) {
+template <typename T, int D, uint32_t GROUPS, uint32_t KEEP, bool ONE, uint32_t WAVES>
+__global__ __launch_bounds__(WAVES * kWaveSize) void choose_tile_kernel(ChooseArgs a) {
+  constexpr uint32_t kTileThreads = WAVES * kWaveSize, kTileWaves = WAVES;
   constexpr uint32_t kTokens = ONE ? 1u : GROUPS * 16u;
   __shared__ __attribute__((aligned(16))) int8_t codes[kTokens * code_row(D)];
-  __shared__ __attribute__((aligned(16))) PickSpace space[ONE ? 1u : kTileWaves];
+  __shared__ __attribute__((aligned(16))) PickSpace<ONE ? kTileWaves : 1u> space[ONE ? 1u : kTileWaves];
   // four words between the tokens, so that 16 of them with four scores each meet every bank once
   constexpr uint32_t kNext = KEEP * kWaveSize * (ONE ? kTileWaves : 1u) + 4u;
   __shared__ __attribute__((aligned(16))) int32_t scores[kTokens * kNext];
@@ -382,7 +391,7 @@ __global__ __launch_bounds__(kTileThreads) void choose_tile_kernel(ChooseArgs a)
   score_pages<D, GROUPS, kTileWaves>(
       a, t, head, lane, wave, codes, begin, end,
       [&]() {
-        if (begin < end) query_codes<T, D, ONE ? 1u : GROUPS * 2u>(a, t, head, lane, wave, kTileWaves, codes);
+        if (begin < end) query_codes<T, D, ONE ? 1u : kTokens / WAVES>(a, t, head, lane, wave, kTileWaves, codes);
         __syncthreads();
       },
       [&](uint32_t token, uint32_t j, i32x4 s) { *reinterpret_cast<i32x4*>(scores + token * kNext + j) = s; });
@@ -414,26 +423,63 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(ChooseArgs a, uint
       [&](uint32_t token, uint32_t j, i32x4 s) { *reinterpret_cast<i32x4*>(scores + token * next_token + j) = s; });
 }
 
-constexpr uint32_t kPickWaves = 16;
-template <uint32_t KEEP>
-__global__ __launch_bounds__(kPickWaves * kWaveSize) void choose_kernel(ChooseArgs a) {
-  __shared__ __attribute__((aligned(16))) PickSpace space;
+template <uint32_t WAVES, uint32_t KEEP>
+__global__ __launch_bounds__(WAVES * kWaveSize) void choose_kernel(ChooseArgs a) {
+  __shared__ __attribute__((aligned(16))) PickSpace<WAVES> space;
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
   const uint32_t pairs = a.per * a.p.kv_heads, tile = blockIdx.x / pairs, in_tile = blockIdx.x % pairs;
   const uint32_t token = in_tile / a.p.kv_heads, head = in_tile % a.p.kv_heads;
   const QueryTile t = query_tile(a, a.first_tile + tile, lane, in_tile == 0u && threadIdx.x == 0u);
   if (token >= t.here) return;
   const int32_t* entries = a.p.table + (uint64_t)t.row * a.p.row_pages;
-  pick<kPickWaves, KEEP, false>(a, lane, wave, in_sight(a, t.base + (int32_t)token), space, a.scores + (((uint64_t)tile * a.per + token) * a.p.kv_heads + head) * a.stride,
+  pick<WAVES, KEEP, false>(a, lane, wave, in_sight(a, t.base + (int32_t)token), space, a.scores + (((uint64_t)tile * a.per + token) * a.p.kv_heads + head) * a.stride,
                          a.choice + ((uint64_t)(t.query + token) * a.p.kv_heads + head) * a.words, [&](uint32_t j) { return (uint32_t)entries[j] < a.p.pages ? kAlways : kAbsent; });
 }
 
+template <uint32_t WAVES, uint32_t KEEP>
+hipError_t launch_pick_of(const ChooseArgs& a, uint32_t units, hipStream_t stream) {
+  choose_kernel<WAVES, KEEP><<<units, WAVES * kWaveSize, 0, stream>>>(a);
+  return hipGetLastError();
+}
+// Blocks of 64 pages a wave keeps: those it has not are looked at too (8193 pages of one token: 5.9 us with 9, 7.6 with 16).  Where there are many (token, kv head)
+// pairs each has as few waves as can keep its scores: less is waited for.
+hipError_t launch_pick(const ChooseArgs& a, uint32_t units, hipStream_t stream) {
+  const uint32_t blocks = a.stride / 64u;
+  if (units >= 2048u && blocks <= 256u) {
+    if (blocks <= 16u) return launch_pick_of<1u, 16u>(a, units, stream);
+    if (blocks <= 24u) return launch_pick_of<1u, 24u>(a, units, stream);
+    if (blocks <= 32u) return launch_pick_of<2u, 16u>(a, units, stream);
+    if (blocks <= 48u) return launch_pick_of<2u, 24u>(a, units, stream);
+    if (blocks <= 64u) return launch_pick_of<2u, 32u>(a, units, stream);
+    if (blocks <= 96u) return launch_pick_of<4u, 24u>(a, units, stream);
+    if (blocks <= 128u) return launch_pick_of<4u, 32u>(a, units, stream);
+    if (blocks <= 192u) return launch_pick_of<8u, 24u>(a, units, stream);
+    return launch_pick_of<8u, 32u>(a, units, stream);
+  }
+  if (blocks <= 64u) return launch_pick_of<16u, 4u>(a, units, stream);
+  if (blocks <= 144u) return launch_pick_of<16u, 9u>(a, units, stream);
+  if (blocks <= 256u) return launch_pick_of<16u, 16u>(a, units, stream);
+  return launch_pick_of<16u, 0u>(a, units, stream);
+}
+
+template <typename T, int D, uint32_t GROUPS, uint32_t KEEP, bool ONE, uint32_t WAVES>
+void launch_tile(const ChooseArgs& a, hipStream_t stream) {
+  choose_tile_kernel<T, D, GROUPS, KEEP, ONE, WAVES><<<a.tiles * a.p.kv_heads, WAVES * kWaveSize, 0, stream>>>(a);
+}
+// Waves of a workgroup and blocks of 64 pages each of them keeps: 2048 pages for a token that all waves share, 384 for 32 tokens, up to 1536 for 16.  16 waves, a token each, where
+// only one workgroup fits a CU or there are no more than two for each (120 tokens of 700 pages 12.7 us, with 8 waves 14.5; 6000 tokens 87, with 8 71).
 template <typename T, int D, uint32_t GROUPS, bool ONE>
 hipError_t launch_tiles(const ChooseArgs& a, hipStream_t stream) {
-  const dim3 grid(a.tiles * a.p.kv_heads);
-  // blocks of 64 pages a wave keeps: 2048 pages for a token that all waves share, 384 for 32 tokens, 768 for 16
-  if constexpr (ONE) choose_tile_kernel<T, D, GROUPS, 4u, ONE><<<grid, kTileThreads, 0, stream>>>(a);
-  else choose_tile_kernel<T, D, GROUPS, GROUPS == 2u ? 6u : 12u, ONE><<<grid, kTileThreads, 0, stream>>>(a);
+  if constexpr (ONE) {
+    launch_tile<T, D, GROUPS, 4u, ONE, 8u>(a, stream);
+  } else if constexpr (GROUPS == 2u) {
+    launch_tile<T, D, GROUPS, 6u, ONE, 8u>(a, stream);
+  } else {
+    if (a.stride > 1024u) launch_tile<T, D, GROUPS, 24u, ONE, 16u>(a, stream);
+    else if (a.stride > 768u) launch_tile<T, D, GROUPS, 16u, ONE, 16u>(a, stream);
+    else if (a.tiles * a.p.kv_heads <= 512u) launch_tile<T, D, GROUPS, 12u, ONE, 16u>(a, stream);
+    else launch_tile<T, D, GROUPS, 12u, ONE, 8u>(a, stream);
+  }
   return hipGetLastError();
 }
 
@@ -453,12 +499,7 @@ hipError_t launch_choose_of(const ChooseArgs& given, hipStream_t stream) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const uint32_t units = a.tiles * a.per * a.p.kv_heads;
-    // blocks of 64 pages a wave keeps: those it has not are looked at too (8193 pages: 5.9 us with 9, 7.6 with 16)
-    if (a.stride <= kPickWaves * 64u * 4u) choose_kernel<4u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
-    else if (a.stride <= kPickWaves * 64u * 9u) choose_kernel<9u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
-    else if (a.stride <= kPickWaves * 64u * 16u) choose_kernel<16u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
-    else choose_kernel<0u><<<units, kPickWaves * kWaveSize, 0, stream>>>(a);
-    e = hipGetLastError();
+    e = launch_pick(a, units, stream);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -9,6 +9,11 @@
 // A tile is what it is in attention over all pages (32 tokens a wave, keys from memory straight into the matrix instruction's operand, weights held to 22 bits,
 // values through the transposing read of LDS; same layouts, same rounding, so results agree to the same bounds).  The waves' sums are joined in LDS, parts by a
 // second kernel.
+//
+// What bounds it: memory where there is much to read, in pieces of a page's rows that lie anywhere.  48 rows with 64 pages of 16 of up to 8192 tokens, 8 kv heads of 128 dimensions: 40.5 us for
+// 194 MB (4.8 TB/s, what a large copy reaches), and the same with keys and values through the caches, with items in the order of the dies, with two parts to an item.  Else
+// the chain lengths - bits - entries - keys - values - two tiles: 131071 tokens of one row, 64 pages of 64: 11.7 us, 7.4 here and 4.3 - 5.1 to join 32 parts.  A row's
+// entries read before the list is known, beside its bits, cost more than the trip to memory that they save (2000 entries of 4 rows: 9.9 us, so 9.5; of 48 rows 45.7, so 44.9).
 #include <algorithm>
 
 #include "paged.h"
@@ -22,7 +27,6 @@ constexpr uint32_t kChosenThreads = 256, kChosenWaves = kChosenThreads / kWaveSi
 constexpr uint32_t kChosenWords = kChosenThreads;        // words of a choice that are turned into a list at a time
 constexpr uint32_t kChosenPages = kChosenWords * 32u;
 constexpr uint32_t kNoPage = 0xFFFFFFFFu;
-constexpr uint32_t kChosenTable = 2048;                  // entries of a row, up to which they are read beside lengths and bits: one trip to memory less in front of the keys
 
 // RUN: tokens of a tile that surely lie in one page: 32, or 1 where pages are smaller.
 template <typename T, int D, uint32_t RUN>
@@ -32,8 +36,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
   constexpr uint32_t kRowLanes = D / 8, kRowsAtOnce = kWaveSize / kRowLanes;
   __shared__ __attribute__((aligned(256))) uint8_t lds[kChosenWaves][kAttendTile * D * 2];      // values, then the waves' sums: 16 heads of D floats
   static_assert(kAttendTile * D * 2 == 16 * D * 4);
-  __shared__ uint32_t list[kChosenPages];                              // and behind kChosenTable of them a row's entries, where it has no more
-  static_assert(kChosenPages >= 2u * kChosenTable);
+  __shared__ uint32_t list[kChosenPages];
   __shared__ f32x2 tops[kChosenWaves][16];
   __shared__ uint32_t counts[2][kChosenWaves];
   const uint32_t lane = threadIdx.x % kWaveSize, wave = (uint32_t)__builtin_amdgcn_readfirstlane((int)(threadIdx.x / kWaveSize));
@@ -54,17 +57,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
     return rest < 32u ? x & ((1u << rest) - 1u) : x;
   };
   const auto word_at = [&](uint32_t w) -> uint32_t { return w * 32u < all ? in_sight(w, bits[w]) : 0u; };
-  const bool staged = a.p.row_pages <= kChosenTable;
   const uint32_t first_bits = threadIdx.x < a.words ? bits[threadIdx.x] : 0u;
-  if (staged) {
-    uint32_t x[kChosenTable / kChosenThreads];
-#pragma unroll
-    for (uint32_t i = 0; i < kChosenTable / kChosenThreads; ++i)
-      if (i * kChosenThreads < a.p.row_pages) x[i] = (uint32_t)entries[min(i * kChosenThreads + threadIdx.x, a.p.row_pages - 1u)];
-#pragma unroll
-    for (uint32_t i = 0; i < kChosenTable / kChosenThreads; ++i)
-      if (i * kChosenThreads < a.p.row_pages) list[kChosenTable + i * kChosenThreads + threadIdx.x] = x[i];
-  }
   typename T::x8 q[kSteps];
 #pragma unroll
   for (uint32_t k = 0; k < kSteps; ++k) {
@@ -100,7 +93,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
     const bool own = total != 0u && list[total - 1u] == all - 1u;      // the page that need not be full is the last one
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < total; i += kChosenThreads) {
-      const uint32_t page = staged ? list[kChosenTable + list[i]] : (uint32_t)entries[list[i]];
+      const uint32_t page = (uint32_t)entries[list[i]];
       list[i] = page < a.p.pages ? page : kNoPage;
       if (page >= a.p.pages) flag(a.status, QKV_STATUS_BAD_PAGE);
     }

@@ -94,6 +94,22 @@ def test_many_pages(pages):
     x.check(1000, 1, 1)
 
 
+@pytest.mark.parametrize("pages", [700, 1000, 1500, 2000, 3000, 4090, 6000, 8190, 12000, 16300])
+@pytest.mark.parametrize("heads,tokens", [(4, 600), (16, 800)])
+def test_many_tokens_with_many_pages(pages, heads, tokens):
+    """Thousands of choices at a time, some of them against the definition; all of them have as many pages as they should."""
+    tokens = min(tokens, pages)
+    x = Scored([pages], heads, 1, 64, 1, new=[tokens], seed=pages)
+    got = x.run(150, 2, 3)
+    assert all(len(one) == min(150, place + 1) for token, place in zip(got, x.places) for one in token)
+    some = sorted({0, 1, 15, 16, 63, 64, tokens - 1} | set(range(5, tokens, 61)))
+    table, digest = x.cache.gtable.cpu().numpy(), x.gdigest.cpu().numpy()
+    for i in some:
+        for h in range(0, heads, 3):
+            assert got[i][h] == chosen_ref.choose(x.q[i, h:h + 1].float().numpy(), x.places[i], 1, table[0], digest.shape[1], digest[0, :, h],
+                                                  x.exponents[0, h].numpy(), 150, 2, 3), (i, h)
+
+
 def test_more_pages_than_registers_hold():
     x = Scored([17000], 1, 1, 64, 1, seed=1)
     x.check(2000, 1, 1)
