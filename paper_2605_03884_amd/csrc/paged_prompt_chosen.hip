@@ -11,6 +11,14 @@
 //            lane 32 further on the other 16), what a pair has not chosen or does not see set to -inf, weights relative to a maximum that follows the true
 //            one only when that has grown by 2^8, O^T = V^T P^T with the weights where the product wants them and V^T through the transposing read of LDS.
 // Weights are rounded to the cache's type, as the result is; maxima, sums and results are in 32 bits.
+//
+// What bounds it: a wave's own chain of scores, maximum, weights and values, with two waves a SIMD (256 registers each).  8192 tokens of 32 heads and 128 dimensions, each at 16 pages of 64: 315 us; the
+// choices ask for 125 GFLOP, a wave's 8 tokens together for 181 (22 pages of the 64 in sight on average, the workgroup's 32 tokens for 27), so matrix units see 0.57 PFLOP/s, busy 24 % of the
+// cycles, vector instructions issuing in 37 %, waves waiting 38 %.  Not memory: with every entry naming the same page it takes as long.  Staging alone takes 155 us, lists, queries and results 48.
+// 1000 tokens of 64 heads of 64 dimensions behind 32768, 64 pages of 32 each: 149 us in three parts, of which 11 join them (33 GFLOP asked for, 46 done).  38 - 150 tokens of six short
+// sequences: 25 us, about 9 and 3 more for each 64 keys that follow each other.
+// What was worth it: waves leave out halves and 64 keys a tile in place of 32 with all waves at all of them 376 -> 315 and 207 -> 176, then parts 149.  And what was not: 8 waves for 256 pairs 348, two
+// tiles' halves in one stream of instructions 332, the next half's scores beside these weights 333, staging between halves 321, four halves deep 733 (registers in memory).
 #include "paged_prompt.h"
 
 namespace qkv {
