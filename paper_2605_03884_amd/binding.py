@@ -121,6 +121,7 @@ class Pages(ctypes.Structure):
                 table.data_ptr(), lens.data_ptr(), None if refs is None else refs.data_ptr())
         p.tensors = (list(k_layers), list(v_layers), table, lens, refs, pointers)
         p.dtype, p.device = first.dtype, first.device
+        p.pool = (first.device, count, *first.shape)
         return p
 
 
@@ -158,6 +159,7 @@ class Digests(ctypes.Structure):
         at = _of_pages(exponents, pages, torch.int8, (pages.layers, pages.kv_heads, pages.head_dim), "exponents")
         d = cls(ctypes.cast(pointers, ctypes.POINTER(ctypes.c_void_p)), at)
         d.tensors = (list(layers), exponents, pointers)
+        d.pool = pages.pool
         return d
 
 
@@ -720,13 +722,19 @@ def paged_prompt(pages, q, starts, softmax_scale, out, lse=None, layer=0, window
     return out, lse
 
 
+def _digests_of(pages, digests):
+    if digests.pool != pages.pool:
+        raise ValueError("these are the digests of a pool of another shape or device")
+    return digests
+
+
 def pages_digest(pages, digests, layer=0, count=1, starts=None, tokens=None, status=None, stream=None):
     """Digests of the pages that new tokens have filled, in layers `layer` .. `layer + count - 1`; starts: device int32 [rows + 1] and the tokens of the
     batch (as many as starts ends with, or more), or None for one token a row."""
     if starts is None and tokens is not None and tokens != pages.rows or starts is not None and tokens is None:
         raise ValueError("tokens is the size of the batch that starts describes")
     at = None if starts is None else _of_pages(starts, pages, torch.int32, (pages.rows + 1,), "starts")
-    _check(lib().qkv_pages_digest(pages, digests, at, pages.rows if tokens is None else tokens, layer, count, _status_of_pages(status, pages), _here(pages, stream)),
+    _check(lib().qkv_pages_digest(pages, _digests_of(pages, digests), at, pages.rows if tokens is None else tokens, layer, count, _status_of_pages(status, pages), _here(pages, stream)),
            "qkv_pages_digest")
 
 
@@ -760,7 +768,7 @@ def paged_choose(pages, digests, q, most, choice=None, first=1, last=1, layer=0,
     x.workspace_dev, x.workspace_bytes = _of_pages(workspace, pages, torch.uint8, workspace.shape, "workspace"), workspace.numel()
     x.status_dev = _status_of_pages(status, pages)
     x.layer, x.q_heads, x.most, x.first, x.last = layer, shape[1], most, first, last
-    _check(lib().qkv_paged_choose(pages, digests, x, _here(pages, stream)), "qkv_paged_choose")
+    _check(lib().qkv_paged_choose(pages, _digests_of(pages, digests), x, _here(pages, stream)), "qkv_paged_choose")
     return choice
 
 

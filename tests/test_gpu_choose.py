@@ -128,6 +128,20 @@ def test_equal_scores(size, pages):
             x.check(most, 1, 1)
 
 
+@pytest.mark.parametrize("pages,heads,tokens", [(1000, 16, 800), (1500, 16, 800), (2000, 4, 600), (3000, 4, 600), (6000, 4, 600), (12000, 4, 600)])
+def test_equal_scores_of_many_tokens(pages, heads, tokens):
+    some = torch.randint(-128, 128, (2, heads, 2, 64), generator=torch.Generator().manual_seed(1), dtype=torch.int8)
+    x = Scored([pages], heads, 1, 64, 1, new=[tokens], seed=pages)
+    x.gdigest.copy_(some[torch.arange(x.digest.shape[1]) % 2].unsqueeze(0))
+    table, digest = x.cache.gtable.cpu().numpy(), x.gdigest.cpu().numpy()
+    for most in (pages // 5, pages - tokens // 2):
+        got = x.run(most)
+        for i in (0, 100, tokens // 2, tokens - 1):
+            for h in range(0, heads, 3):
+                assert got[i][h] == chosen_ref.choose(x.q[i, h:h + 1].float().numpy(), x.places[i], 1, table[0], digest.shape[1], digest[0, :, h],
+                                                      x.exponents[0, h].numpy(), most, 1, 1), (most, i, h)
+
+
 def test_the_largest_scores():
     """Codes at the ends of their range: scores of plus and minus 127 * 128 * 2 * 256."""
     x = Scored([640], 2, 1, 256, 16, seed=2, spread=0)

@@ -268,3 +268,47 @@ def test_places_next_to_the_largest():
         if i == 2:
             check_attend(host(one), host(one_lse), want, dim, 64)
     assert int(status) == 0
+
+
+def test_tensors_that_are_refused():
+    """On the host, before anything is enqueued."""
+    cache = Cache([40, 3], 2, 64, 16)
+    pages, count = cache.pages, cache.k.shape[1]
+    bounds, exponents = torch.zeros(count, 2, 2, 64, dtype=torch.int8, device="cuda"), torch.zeros(1, 2, 64, dtype=torch.int8, device="cuda")
+    for layers, steps in (([], exponents), ([bounds, bounds], exponents), ([bounds[1:]], exponents), ([bounds.short()], exponents), ([bounds.cpu()], exponents),
+                          ([bounds.transpose(2, 3).contiguous().transpose(2, 3)], exponents), ([bounds], exponents[0]), ([bounds], exponents.int()), ([bounds], exponents.cpu())):
+        with pytest.raises(ValueError):
+            qkv.Digests.make(pages, layers, steps)
+    digests = qkv.Digests.make(pages, [bounds], exponents)
+    other = Cache([40, 3], 2, 64, 16, spare=9)
+    q, words = torch.zeros(2, 4, 64, dtype=torch.float16, device="cuda"), torch.zeros(2, 2, 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        qkv.pages_digest(other.pages, digests)
+    with pytest.raises(ValueError):
+        qkv.paged_choose(other.pages, digests, q, 3)
+    for bad in (dict(starts=ints(0, 1, 2)), dict(tokens=3), dict(starts=ints(0, 1), tokens=2), dict(starts=ints(0, 1, 2).long(), tokens=2),
+                dict(status=torch.zeros(1, dtype=torch.int64, device="cuda"))):
+        with pytest.raises(ValueError):
+            qkv.pages_digest(pages, digests, **bad)
+    for bad in (dict(q=q.float()), dict(q=q[..., :32]), dict(q=q[0]), dict(q=q.transpose(1, 2).contiguous().transpose(1, 2)), dict(choice=words[:1]), dict(choice=words.long()),
+                dict(starts=ints(0, 2)), dict(workspace=torch.zeros(8, device="cuda"))):
+        with pytest.raises(ValueError):
+            qkv.paged_choose(**{"pages": pages, "digests": digests, "q": q, "most": 3, **bad})
+    for bad in (dict(most=1), dict(last=0), dict(layer=1), dict(q=q[:1]), dict(q=q[:, :3])):
+        with pytest.raises(qkv.QkvError):
+            qkv.paged_choose(**{"pages": pages, "digests": digests, "q": q, "most": 3, **bad})
+    out = torch.zeros(2, 4, 64, device="cuda")
+    for bad in (dict(choice=words.long()), dict(choice=words[:, :1]), dict(choice=words.expand(2, 2, 2)), dict(q=q.float()), dict(out=out.half()),
+                dict(prior=(out, out)), dict(lse=out)):
+        with pytest.raises(ValueError):
+            qkv.paged_attend_chosen(**{"pages": pages, "choice": words, "q": q, "softmax_scale": 0.1, "out": out, **bad})
+        if "prior" not in bad:
+            with pytest.raises(ValueError):
+                more = {**bad, "out": out} if "out" in bad else bad
+                qkv.paged_prompt_chosen(**{"pages": pages, "choice": words, "q": q, "softmax_scale": 0.1, "out": out.half(), "starts": ints(0, 1, 2), **more})
+    with pytest.raises(ValueError):
+        qkv.paged_prompt_chosen(pages, words, q, ints(0, 2), 0.1, out.half())
+    starts, row = ints(0, 0, 0), ints(0, 0)
+    for bad in (dict(), dict(row=row, tokens=3), dict(row=row.long()), dict(row=row, place=ints(0)), dict(slot=row), dict(row=row, more=ints(1))):
+        with pytest.raises(ValueError):
+            qkv.pages_slots(pages, starts, **bad)
