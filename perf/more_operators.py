@@ -221,6 +221,7 @@ def prepare(case, seed):
         state["pages"] = qkv.Pages.make(list(state["k"]), list(state["v"]), table, state["lens"])
         if op in ("digest", "choose"):
             state["digests"] = qkv.Digests.make(state["pages"], list(state["digest"]), state["exponents"])
+            state["batch"] = None if new is None else tokens      # a caller knows the size of its batch
         size_of = {"choose": lambda: qkv.paged_choose_workspace(state["pages"], tokens),
                    "attend": lambda: qkv.paged_attend_chosen_workspace(state["pages"], case["q_heads"], case["most"]),
                    "prompt": lambda: qkv.paged_prompt_chosen_workspace(state["pages"], case["q_heads"], tokens)}.get(op)
@@ -384,8 +385,7 @@ def _run_own(s, case):
     import paper_2605_03884_amd as qkv
     op, pages, status = case["op"], s["pages"], s["status"]
     if op == "digest":
-        qkv.pages_digest(pages, s["digests"], count=case["layers"], starts=s["starts"],
-                         tokens=None if s["starts"] is None else sum(_plan(case)[1]), status=status)
+        qkv.pages_digest(pages, s["digests"], count=case["layers"], starts=s["starts"], tokens=s["batch"], status=status)
         return s["digest"]
     if op == "choose":
         return qkv.paged_choose(pages, s["digests"], s["q"], case["most"], s["choice"], first=case["first"], last=case["last"], starts=s["starts"],
