@@ -29,7 +29,7 @@ constexpr uint32_t kKeys = 64;                           // of a tile
 constexpr uint32_t kListWords = 64;                      // words of a choice that are made into a list at a time, a lane each
 constexpr uint32_t kListSpans = kListWords * 32u;        // a span: a page, or the 32 keys of as many pages as hold them
 constexpr uint32_t kEvery = 0x8000u;                     // in the list: all tokens of the workgroup have chosen it
-constexpr int32_t kNowhere = 0x7FFFFF80;                 // a half behind the list: keys that nobody sees
+constexpr int32_t kNowhere = -32;                        // a half behind the list: keys that nobody sees, in unsigned numbers behind every place
 
 // Waves a SIMD holds at once: what its 512 registers allow.
 constexpr uint32_t waves_a_simd(int D) { return D == 256 ? 1u : D == 128 ? 2u : 3u; }
@@ -213,9 +213,9 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
   const auto key_of = [&](const Tile& t, uint32_t of) -> int32_t { return first_key(of < 32u ? t.half[0] : t.half[1]) + (int32_t)(of % 32u); };
   const auto lanes_key = [&](const Tile& t) -> int32_t { return first_key(lane < 32u ? t.half[0] : t.half[1]) + (int32_t)(lane % 32u); };
   const auto seen_by_some = [&](int32_t key) {
-    if (RUN == 64u || span_pages == 1u) return key < reach;            // a half is one page's
+    if (RUN == 64u || span_pages == 1u) return (uint32_t)key < (uint32_t)reach;      // a half is one page's
     const uint32_t page = (uint32_t)key >> page_shift;
-    return key < reach && (by_some[page / 32u - first_word] >> (page % 32u) & 1u) != 0u;
+    return (uint32_t)key < (uint32_t)reach && (by_some[page / 32u - first_word] >> (page % 32u) & 1u) != 0u;
   };
   const auto look_up = [&](const Tile& t) -> uint32_t { return (uint32_t)entries[min((uint32_t)lanes_key(t), (uint32_t)reach - 1u) >> page_shift]; };
   // Where the thread's rows of a tile are, in head 0: with pages of at least RUN tokens a place for each load that is the same for the wave, to which `own` is
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
   };
   const auto store_values = [&](const Tile& t, uint32_t place) {
     // Rows that nobody sees may hold anything: behind the sequence nothing has been written yet.
-    const bool cut = first_key(t.half[1]) > reach - 32 || (RUN != 64u && span_pages != 1u);
+    const bool cut = (uint32_t)first_key(t.half[1]) + 31u >= (uint32_t)reach || (RUN != 64u && span_pages != 1u);
 #pragma unroll
     for (uint32_t j = 0; j < kLoads; ++j) {
       if (cut && !seen_by_some(key_of(t, j * kRowsAtOnce + my_row))) vx[j] = (u32x4)(0u);
@@ -388,7 +388,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
 #pragma unroll
       for (uint32_t half = 0; half < 2u; ++half) {
         const int32_t t = first_key(now.half[half]);
-        if (t >= reach || __builtin_amdgcn_ballot_w64(live && (bits[half] >> ((uint32_t)t >> page_shift) % 32u & span_mask) != 0u) == 0ull) continue;
+        if ((uint32_t)t >= (uint32_t)reach || __builtin_amdgcn_ballot_w64(live && (bits[half] >> ((uint32_t)t >> page_shift) % 32u & span_mask) != 0u) == 0ull) continue;
         const uint8_t *const k_at = k_place[place] + half * 32u * key_row(D), *const v_at = v_place[place] + half * 32u * value_row(D);
         f32x16 s = (f32x16)(0.0f);
 #pragma unroll
@@ -440,7 +440,7 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
         const Tile tile = tile_of(i);
         for (uint32_t of = 0; of < kKeys; ++of) {
           const int32_t key = key_of(tile, of);
-          if (key >= reach) continue;
+          if ((uint32_t)key >= (uint32_t)reach) continue;
           const uint32_t page = (uint32_t)key >> page_shift, entry = (uint32_t)entries[page];
           if (entry >= a.p.pages) continue;
           const uint64_t row_at = (uint64_t)entry * a.p.page_stride + (uint64_t)((uint32_t)key & in_page) * a.p.token_stride;

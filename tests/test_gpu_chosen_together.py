@@ -270,6 +270,29 @@ def test_places_next_to_the_largest():
     assert int(status) == 0
 
 
+def test_odd_lists_next_to_the_largest():
+    """What stands for a half of a tile that a list of odd length has not is behind every place there may be."""
+    size, row_pages, heads, dim = 16, (1 << 27) - 2, 1, 64
+    gen = torch.Generator().manual_seed(10)
+    k, v = (torch.randn(4, heads, size, dim, generator=gen).half() for _ in range(2))
+    table = (torch.arange(row_pages, device="cuda", dtype=torch.int32) % 4).view(1, -1)
+    p = qkv.Pages.make([k.cuda()], [v.cuda()], table, ints(row_pages * size))
+    near = set(range(row_pages - 10, row_pages - 2))                   # pages of 2^31 - 192 and on
+    chosen = [{1 << 26} | near, {1 << 26}, near - {row_pages - 8}]
+    words = torch.zeros(3, heads, (row_pages + 31) // 32, dtype=torch.int32, device="cuda")
+    for i, some in enumerate(chosen):
+        for j in some:
+            words[i, 0, j // 32] |= (1 << (j % 32)) - (1 << 32 if j % 32 == 31 else 0)
+    q = torch.randn(3, 2, dim, generator=gen).half()
+    out, lse = torch.empty(3, 2, dim, dtype=torch.float16, device="cuda"), torch.empty(3, 2, device="cuda")
+    qkv.paged_prompt_chosen(p, words, q.cuda(), ints(0, 3), 0.125, out, lse)
+    for i in range(3):
+        tokens = [t for j in sorted(chosen[i]) for t in range(j * size, (j + 1) * size)]
+        K, V = (torch.stack([x[(t // size) % 4, 0, t % size] for t in tokens]).double().numpy()[None] for x in (k, v))
+        want = paged_ref.attend(q[i:i + 1].double().numpy(), K, V, [len(tokens) - 1], 0.125)
+        check_prompt(host(out)[i:i + 1], host(lse)[i:i + 1], want, dim, 64, "fp16", 6.0)
+
+
 def test_tensors_that_are_refused():
     """On the host, before anything is enqueued."""
     cache = Cache([40, 3], 2, 64, 16)
