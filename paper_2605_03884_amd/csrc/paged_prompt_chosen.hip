@@ -420,7 +420,8 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
   if ((special & kLost) != 0u && lane == 0u) flag(a.status, QKV_STATUS_BAD_PAGE);
 
   // Values that are infinite or no number have spoilt their dimension for all pairs that met them, with a weight of nothing too.  Where that has happened a pair goes
-  // through its keys once more, one by one: values that are numbers count with their weights, the others as they are.
+  // through its keys once more: values that are numbers count with their weights, the others as they are.  Scores are the same products as before, to the bit: m and l
+  // are made of those, and two sums in another order are a factor of 2^several apart where scores are beyond 2^24.
   f32x16 zero = (f32x16)(0.0f);                                        // stays that only where all are numbers
 #pragma unroll
   for (uint32_t d = 0; d < kSlabs; ++d) zero += acc[d] * 0.0f;
@@ -433,41 +434,51 @@ __global__ __launch_bounds__(kThreads, waves_a_simd(D)) void prompt_chosen_kerne
 #pragma unroll
       for (uint32_t d = 0; d < kSlabs; ++d) acc[d] = (f32x16)(0.0f);
     }
+    static_assert(kWaves * 32u * 32u * 4u <= sizeof(v_place));
+    float* const weights = reinterpret_cast<float*>(v_place[0]) + wave * 1024u;      // the wave's: of 32 keys, 32 pairs each; nobody reads values there any more
     for (first_word = 0u; first_word * 32u < in_sight; first_word += kListWords) {
       make_list();
       const uint32_t tiles = (units + kTileUnits - 1u) / kTileUnits, last = (uint32_t)((uint64_t)tiles * (blockIdx.y + 1u) / a.splits);
       for (uint32_t i = (uint32_t)((uint64_t)tiles * blockIdx.y / a.splits); i < last; ++i) {
         fill_window(i * kTileUnits);
         const Tile tile = tile_of(i);
-        for (uint32_t of = 0; of < kKeys; ++of) {
-          const int32_t key = key_of(tile, of);
-          if ((uint32_t)key >= (uint32_t)reach) continue;
-          const uint32_t page = (uint32_t)key >> page_shift, entry = (uint32_t)entries[page];
-          if (entry >= a.p.pages) continue;
-          const uint64_t row_at = (uint64_t)entry * a.p.page_stride + (uint64_t)((uint32_t)key & in_page) * a.p.token_stride;
-          float s = 0.0f;
 #pragma unroll 1
+        for (uint32_t half = 0; half < 2u; ++half) {
+          const int32_t t = first_key(tile.half[half]);
+          if ((uint32_t)t >= (uint32_t)reach) continue;
+          const uint32_t key = min((uint32_t)t + n, (uint32_t)reach - 1u), entry = (uint32_t)entries[key >> page_shift];      // the lane's row of K
+          const uint8_t* from = keys + (uint64_t)(entry < a.p.pages ? entry : 0u) * a.p.page_stride + (uint64_t)(key & in_page) * a.p.token_stride + h * 16u;
+          f32x16 s = (f32x16)(0.0f);
+#pragma unroll
           for (uint32_t k = 0; k < kSteps; ++k) {
-            const typename T::x8 x = *reinterpret_cast<const typename T::x8*>(keys + row_at + (k * 2u + h) * 16u);
             u32x4 y = (u32x4)(0u);
             if (live) y = *reinterpret_cast<const u32x4*>(a.q + query * a.q_token_stride + (uint64_t)hq * a.q_head_stride + (k * 16u + h * 8u) * 2u);
-            const typename T::x8 z = __builtin_bit_cast(typename T::x8, y);
-#pragma unroll
-            for (uint32_t j = 0; j < 8u; ++j) s = __builtin_fmaf((float)x[j], (float)z[j], s);
+            if (a.flip) y ^= (u32x4)(0x80008000u);
+            s = T::mfma32(__builtin_bit_cast(typename T::x8, *reinterpret_cast<const u32x4*>(from + k * 32u)), __builtin_bit_cast(typename T::x8, y), s);
           }
-          s = sum32(s);
-          if (!spoilt || key > mine || (words[page / 32u] >> (page % 32u) & 1u) == 0u) continue;
-          if (a.flip) s = -s;
           if ((special & kScaled) != 0u) s *= a.scale_log2;
-          const float weight = (float)(typename T::one)exp2f_(__builtin_fmaf(s, scale, -less));
 #pragma unroll
-          for (uint32_t d = 0; d < kSlabs; ++d)
+          for (uint32_t j = 0; j < 16u; ++j) weights[(8u * (j / 4u) + 4u * h + j % 4u) * 32u + n] = (float)(typename T::one)exp2f_(__builtin_fmaf(s[j], scale, -less));
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+          for (uint32_t of = 0; of < 32u && (uint32_t)t + of < (uint32_t)reach; ++of) {
+            const uint32_t at_key = (uint32_t)t + of, page = at_key >> page_shift, number = (uint32_t)entries[page];
+            if (number >= a.p.pages) continue;
+            if (!spoilt || (int32_t)at_key > mine || (words[page / 32u] >> (page % 32u) & 1u) == 0u) continue;
+            const uint64_t row_at = (uint64_t)number * a.p.page_stride + (uint64_t)(at_key & in_page) * a.p.token_stride;
+            const float weight = weights[of * 32u + n];
 #pragma unroll
-            for (uint32_t j = 0; j < 4u; ++j) {
-              const typename T::x4 v = *reinterpret_cast<const typename T::x4*>(values + row_at + (d * 32u + j * 8u + h * 4u) * 2u);
+            for (uint32_t d = 0; d < kSlabs; ++d)
 #pragma unroll
-              for (uint32_t e = 0; e < 4u; ++e) acc[d][4u * j + e] += __builtin_fabsf((float)v[e]) < INFINITY ? (float)v[e] * weight : (float)v[e];
-            }
+              for (uint32_t j = 0; j < 4u; ++j) {
+                const typename T::x4 v = *reinterpret_cast<const typename T::x4*>(values + row_at + (d * 32u + j * 8u + h * 4u) * 2u);
+#pragma unroll
+                for (uint32_t e = 0; e < 4u; ++e) acc[d][4u * j + e] += __builtin_fabsf((float)v[e]) < INFINITY ? (float)v[e] * weight : (float)v[e];
+              }
+          }
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // the next half's weights take these ones' place
+          __builtin_amdgcn_wave_barrier();
         }
       }
     }
