@@ -262,10 +262,11 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
 #pragma unroll
     for (uint32_t w = 0; w < kChosenWaves; ++w) {
       const f32x2 ml = tops[w][h];
-      const float take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);                // no weight, but what is infinite in it is seen
+      const float take = ml.x == -INFINITY ? 0.0f : exp2f_(ml.x - top);
       sum += ml.y * take;
       o += *reinterpret_cast<const f32x4*>(lds[w] + (h * D + at * 4u) * 4u) * take;
     }
+    keep_odd(o, kChosenWaves, [&](uint32_t w) { return *reinterpret_cast<const f32x4*>(lds[w] + (h * D + at * 4u) * 4u); });
     if (a.parts != 1u) {
       const uint64_t slot = ((uint64_t)item * a.parts + blockIdx.y) * min(16u, a.rep) + h;
       *reinterpret_cast<f32x4*>(a.part_o + slot * D + at * 4u) = o;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(kChosenThreads, D == 256 ? 1 : 2) void chosen_kerne
     float lse = top == -INFINITY ? -INFINITY : (top - T::kLift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
     float other = 0.0f;
     if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
-    o *= scale;
+    o = weighed(o, scale);
     if (a.prior_out && other != 0.0f) o += *reinterpret_cast<const f32x4*>(a.prior_out + at_head * D + at * 4u) * other;
     *reinterpret_cast<f32x4*>(a.out + at_head * D + at * 4u) = o;
     if (a.lse && at == 0u) a.lse[at_head] = lse;
@@ -319,12 +320,13 @@ __global__ __launch_bounds__(kChosenJoin) void chosen_join_kernel(ChosenAttendAr
     }
     m = top;
   }
+  keep_odd(o, a.parts, [&](uint32_t s) { return *reinterpret_cast<const f32x4*>(a.part_o + (((uint64_t)item * a.parts + s) * heads + h) * D + at * 4u); });
   const uint64_t at_head = (uint64_t)row * a.p.kv_heads * a.rep + (inner / a.blocks) * a.rep + block * 16u + h;
   float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
   float lse = m == -INFINITY ? -INFINITY : (m - lift + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   float other = 0.0f;
   if (a.prior_out) join(lse, a.prior_lse[at_head], scale, other);
-  o *= scale;
+  o = weighed(o, scale);
   if (a.prior_out && other != 0.0f) o += *reinterpret_cast<const f32x4*>(a.prior_out + at_head * D + at * 4u) * other;
   *reinterpret_cast<f32x4*>(a.out + at_head * D + at * 4u) = o;
   if (a.lse && at == 0u) a.lse[at_head] = lse;

@@ -549,6 +549,7 @@ __global__ __launch_bounds__(kJoinThreads) void prompt_chosen_join_kernel(PagedP
     }
     m = top;
   }
+  keep_odd(o, a.splits, [&](uint32_t s) { return *reinterpret_cast<const f32x4*>(a.part_o + (s * all + pair) * D + at * 4u); });
   const float scale = l == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(l);
   typename T::x4 r;
 #pragma unroll

@@ -46,6 +46,30 @@ __device__ inline uint32_t value_turn(uint32_t token) {
   return D == 64 ? (token >> 1) & 3u : token & 7u;
 }
 
+// What is infinite or no number in the sums that parts of the keys have, of which `o` is the join by their weights: it stays that where a part weighs nothing.  0 times
+// infinity is no number, and whether a value has no weight by itself or its part has none depends on how the keys were cut.  `part(i)`: the sums of part i < n.
+template <typename Part>
+__device__ inline void keep_odd(f32x4& o, uint32_t n, Part part) {
+  const f32x4 zero = o * 0.0f;
+  if (__builtin_expect(zero.x + zero.y + zero.z + zero.w == 0.0f, 1)) return;
+  f32x4 odd = (f32x4)(0.0f);
+  for (uint32_t i = 0; i < n; ++i) {
+    const f32x4 x = part(i);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (!(__builtin_fabsf(x[k]) < INFINITY)) odd[k] += x[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (!(__builtin_fabsf(odd[k]) < INFINITY)) o[k] = odd[k];
+}
+// The same for a join's last factor, which is nothing where what it is joined with has all the weight.
+__device__ inline f32x4 weighed(f32x4 o, float weight) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = __builtin_fabsf(o[k]) < INFINITY ? o[k] * weight : o[k];
+  return o;
+}
+
 // Joins a result (lse, factor `scale` of its sums) with another one of log-sum `other_lse`: afterwards lse is that of both, and the
 // result is the sums times `scale` plus the other one times `other`.
 __device__ inline void join(float& lse, float other_lse, float& scale, float& other) {

@@ -84,3 +84,51 @@ def test_the_other_dimensions(kind, size, scale, length, absent):
     assert np.isfinite(out[:, :, rest]).all()
     err = np.abs(out - clean)[:, :, rest]
     assert (err <= bound[:, :, rest]).all(), (err / bound[:, :, rest]).max()
+
+
+def far_apart(length, size, kind, rows=1):
+    """Tokens of the first two pages score lowest by far; the second one holds an infinite value, the last one of the first page something that is no number."""
+    cache = Cache([length] * rows, 1, 64, size, kind, seed=size)
+    cache.k[..., 0] = 8.0
+    for b in range(rows):
+        cache.k[0, cache.table[b, :2].long(), :, :, 0] = -8.0
+        cache.v[0, cache.table[b, 1], 0, 0, ODD[0]] = -float("inf")
+        cache.v[0, cache.table[b, 0], 0, size - 1, ODD[1]] = float("nan")
+    cache.gpu()
+    return cache
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("size", [4, 32, 64])
+@pytest.mark.parametrize("strength", [1.0, 30.0, 1000.0])
+def test_an_infinite_value_without_weight(kind, size, strength):
+    """Weights of 2^-20 down to nothing: the value's dimension is infinite, whichever part of the keys it is in."""
+    length, n = 9000, 40
+    cache = far_apart(length, size, kind)
+    q = torch.randn(n, 4, 64, generator=torch.Generator().manual_seed(2)).to(TYPES[kind])
+    q[:, :, 0] = strength
+    choices = [[{1, (length // 2) // size, (length - n + i) // size} | ({0} if i % 2 else set())] for i in range(n)]
+    out, lse = run(cache, [n], choices, q, 1.0)
+    assert np.isneginf(out[:, :, ODD[0]]).all() and np.isnan(out[1::2, :, ODD[1]]).all() and np.isfinite(out[::2, :, ODD[1]]).all() and np.isfinite(lse).all()
+    assert np.isfinite(out[:, :, [d for d in range(64) if d not in ODD]]).all()
+
+
+@pytest.mark.parametrize("kind", ["fp16", "bf16"])
+@pytest.mark.parametrize("size", [4, 64])
+@pytest.mark.parametrize("strength", [1.0, 30.0, 1000.0])
+@pytest.mark.parametrize("most", [0, 3])
+@pytest.mark.parametrize("prior", [None, 0.0, 1e6])
+def test_an_infinite_value_without_weight_and_single_tokens(kind, size, strength, most, prior):
+    """The same for one token of a sequence, in parts or whole, alone or joined with what weighs as much or more."""
+    rows = 2
+    cache = far_apart(2000, size, kind, rows)
+    q = torch.randn(rows, 4, 64, generator=torch.Generator().manual_seed(2)).to(TYPES[kind])
+    q[:, :, 0] = strength
+    some = {1, 1999 // size} | set(range(8, 1999 // size, 2))
+    words = as_words([[some], [some | {0}]], cache.table.shape[1])
+    out, lse = torch.full((rows, 4, 64), 7.0, device="cuda"), torch.full((rows, 4), 7.0, device="cuda")
+    other = None if prior is None else (torch.ones(rows, 4, 64, device="cuda"), torch.full((rows, 4), 8.0 * strength + prior, device="cuda"))
+    qkv.paged_attend_chosen(cache.pages, words, q.cuda(), 1.0, out, lse, most=most, prior=other)
+    got = out.double().cpu().numpy()
+    assert np.isneginf(got[:, :, ODD[0]]).all() and np.isnan(got[1, :, ODD[1]]).all() and np.isfinite(got[0, :, ODD[1]]).all() and bool(torch.isfinite(lse).all())
+    assert np.isfinite(got[:, :, [d for d in range(64) if d not in ODD]]).all()
