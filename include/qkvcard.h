@@ -687,7 +687,7 @@ int qkv_pages_digest(const qkv_pages_t* pages, const qkv_digests_t* digests, con
  *             the last row's are left as they were.
  *   workspace_dev: device scratch of qkv_paged_choose_workspace() bytes, 16-byte aligned, contents unspecified; NULL where that is 0.  What is named for a number
  *             of tokens is enough for fewer.  Two calls that may run at once need one each.
- * Limits: row_pages < 2^20; tokens * kv_heads * 64 < 2^31; for prompts (tokens / 16 + rows) * kv_heads < 2^23.
+ * Limits: row_pages < 2^20; tokens * kv_heads * 64 < 2^31; rows * kv_heads < 2^23, and for prompts (tokens / 16 + rows) * kv_heads < 2^23.
  * Errors: QKV_ERR_NULL, QKV_ERR_SHAPE, QKV_ERR_ALIGN, QKV_ERR_CAPACITY, QKV_ERR_HIP.
  */
 typedef struct qkv_choose {

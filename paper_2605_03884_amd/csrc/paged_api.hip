@@ -229,12 +229,16 @@ int plan_choose(const qkv_pages_t* p, int64_t tokens, bool single, ChoosePlan& a
   return QKV_OK;
 }
 // What is enough for every batch of up to `tokens`: tiles get larger with their number, and the largest that are cut off at kScoreBytes need not be those of most tokens.
+// As many tokens as there are rows may be one of each where prompts of as many have no room in a launch: then the most that prompts may have counts.
 int most_choose_bytes(const qkv_pages_t* p, int64_t tokens, uint64_t& bytes) {
   bytes = 0u;
-  const int64_t border = 32ll * p->rows - 1;
+  const int64_t border = 32ll * p->rows - 1, most = 16ll * (((1ll << 23) - 1) / p->kv_heads - p->rows) + 15;
   for (int64_t n : {tokens, std::min(tokens, border)}) {
     ChoosePlan plan;
-    const int rc = plan_choose(p, n, false, plan);
+    int rc = plan_choose(p, n, false, plan);
+    if (rc && tokens != p->rows) return rc;
+    if (rc && most < 1) continue;
+    if (rc) rc = plan_choose(p, std::min(n, most), false, plan);
     if (rc) return rc;
     bytes = std::max(bytes, plan.bytes);
   }
