@@ -712,6 +712,9 @@ int qkv_paged_choose(const qkv_pages_t* pages, const qkv_digests_t* digests, con
  * results, rounding, what is not seen, limits, errors - is as it is there; window and sinks are 0 (QKV_ERR_SHAPE).  Any bits will do: none, all, or a choice of the
  * caller's own.  Bits of pages behind a query's own mean nothing, as do those behind row_pages in a last word.
  *   choice_dev: device, uint32_t [tokens][kv_heads][(row_pages + 31) / 32].
+ * Where sequences are short there is little to leave out, and finding it costs more than it saves: of prompts, 510 tokens of six sequences of up to 368 tokens take 25 us
+ * with 8 pages of 16 each, where qkv_paged_prompt takes 17 over all of their tokens, and 1000 tokens behind 4000 58, where it takes 114 (32 / 8 heads of 128 dimensions, the
+ * choice itself not counted; the two are even near 2000 tokens).
  *   most:     how many bits of a query are set, about; 0 if that is not known.  It guides how the work is cut, and decides with the shape how large
  *             the workspace has to be; results are right whatever is set.
  */

@@ -184,8 +184,8 @@ struct PagedPromptArgs {
   float *part_o, *part_ml;                               // [splits][tokens][q heads][dim], [...][2]
   uint32_t splits, least;                                // parts of a query tile's keys at most, keys of a part at least
   uint32_t* status;
-  const uint32_t* choice;                                // pages chosen for each (token, kv head); null where all are seen
-  uint32_t words;                                        // of one
+  const uint32_t* choice;                                // pages chosen for each (token, kv head), and the words of one: attention over chosen pages only
+  uint32_t words;
 };
 
 struct DigestArgs {

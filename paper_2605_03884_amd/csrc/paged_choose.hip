@@ -12,10 +12,11 @@
 // writes the scores of stretches of pages to the workspace and a second one picks.
 //
 // What bounds it: many tokens, instructions.  6583 tokens of two prompts behind up to 8000, pages of 32, 8 kv heads of 128 dimensions: 54.6 us for 58 MB (12 us of a copy) and 7.4 G
-// operations; vector instructions issue in 54 % of the cycles, 373 for each of 52664 choices.  Single tokens, one chain: lengths, entries, digests, scores, picks.  48 rows of up to 8192
+// operations; vector instructions issue in 53 % of the cycles, 373 for each of 52664 choices.  Single tokens, one chain: lengths, entries, digests, scores, picks.  48 rows of up to 8192
 // tokens in pages of 16: 11.6 us for 26 MB; 131071 tokens of one row: 13.3 us for 16.8 MB, 6.2 for the scores and 7 for the picks, which are those of 8 workgroups.
 // What steps were worth, these three: scores in LDS and counting (8 bits a look) in place of bisection over the workspace (a bit a look) 128.6 -> 59, 19.5 -> 12.8 and 22.4 -> 14.6 us; of it no
-// branches in a wave's blocks 70 -> 57 (with 16 tokens a tile 71 where 32 have 57).  A wave or two for each of many choices, in place of 16 that wait for each other: 3000 tokens of 4000 pages 347 -> 202.
+// branches in a wave's blocks 70 -> 57 (with 16 tokens a tile 71 where 32 have 57).  With 256 dimensions the codes of four tokens at once do not fit the registers: tiles of 32 and of 64 tokens keep 224
+// bytes a lane in memory then.  A wave or two for each of many choices, in place of 16 that wait for each other: 3000 tokens of 4000 pages 347 -> 202.
 #include <algorithm>
 
 #include "paged.h"

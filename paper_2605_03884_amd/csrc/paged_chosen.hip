@@ -12,7 +12,7 @@
 //
 // What bounds it: memory where there is much to read, in pieces of a page's rows that lie anywhere.  48 rows with 64 pages of 16 of up to 8192 tokens, 8 kv heads of 128 dimensions: 40.5 us for
 // 194 MB (4.8 TB/s, what a large copy reaches), and the same with keys and values through the caches, with items in the order of the dies, with two parts to an item.  Else
-// the chain lengths - bits - entries - keys - values - two tiles: 131071 tokens of one row, 64 pages of 64: 11.7 us, 7.4 here and 4.3 - 5.1 to join 32 parts.  A row's
+// the chain lengths - bits - entries - keys - values - two tiles: 131071 tokens of one row, 64 pages of 64: 11.8 us, 7.0 here and 4.2 - 5.3 to join 32 parts.  A row's
 // entries read before the list is known, beside its bits, cost more than the trip to memory that they save (2000 entries of 4 rows: 9.9 us, so 9.5; of 48 rows 45.7, so 44.9).
 #include <algorithm>
 

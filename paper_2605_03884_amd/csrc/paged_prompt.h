@@ -1,5 +1,4 @@
-// paged_prompt.h — what the two kernels for many new tokens share: how a running maximum is kept, how rows stand in LDS, what is done with values that are infinite or
-// no number.
+// paged_prompt.h — what the two kernels for many new tokens share: how a running maximum is kept, how rows stand in LDS.
 #pragma once
 
 #include "paged.h"
@@ -21,21 +20,5 @@ __device__ inline float uniform(float x) { return __builtin_bit_cast(float, __bu
 
 constexpr uint32_t key_row(int D) { return D * 2u + 16u; }
 constexpr uint32_t value_row(int D) { return D * 2u + 64u; }
-
-// Takes what is infinite or no number out of eight values; whether there was any.
-template <typename T>
-__device__ inline bool take_out(u32x4& x) {
-  constexpr uint32_t e = T::kExponent;
-  bool any = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    uint32_t keep = 0xFFFFFFFFu;
-    if ((x[i] & e) == e) keep = 0xFFFF0000u;
-    if ((x[i] & (e << 16)) == (e << 16)) keep &= 0xFFFFu;
-    any = any || keep != 0xFFFFFFFFu;
-    x[i] &= keep;
-  }
-  return any;
-}
 
 }  // namespace qkv

@@ -31,6 +31,22 @@ constexpr uint32_t prompt_keys(uint32_t waves) { return waves == 8u ? 64u : 32u;
 // Waves a SIMD holds at once: what its 512 registers allow.
 constexpr uint32_t prompt_waves_a_simd(int D) { return D == 256 ? 1u : D == 128 ? 2u : 3u; }
 
+// Takes what is infinite or no number out of eight values; whether there was any.
+template <typename T>
+__device__ inline bool take_out(u32x4& x) {
+  constexpr uint32_t e = T::kExponent;
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t keep = 0xFFFFFFFFu;
+    if ((x[i] & e) == e) keep = 0xFFFF0000u;
+    if ((x[i] & (e << 16)) == (e << 16)) keep &= 0xFFFFu;
+    any = any || keep != 0xFFFFFFFFu;
+    x[i] &= keep;
+  }
+  return any;
+}
+
 template <typename T, int D, uint32_t RUN, uint32_t WAVES>
 __global__ __launch_bounds__(WAVES * kWaveSize, prompt_waves_a_simd(D)) void prompt_kernel(PagedPromptArgs a) {
   constexpr uint32_t kThreads = WAVES * kWaveSize;

@@ -10,14 +10,18 @@
 //   half     a wave none of whose pairs has chosen it leaves it out.  Otherwise scores S^T = K Q^T on v_mfma_f32_32x32x16 (a lane gets 16 scores of its own pair, the
 //            lane 32 further on the other 16), what a pair has not chosen or does not see set to -inf, weights relative to a maximum that follows the true
 //            one only when that has grown by 2^8, O^T = V^T P^T with the weights where the product wants them and V^T through the transposing read of LDS.
-// Weights are rounded to the cache's type, as the result is; maxima, sums and results are in 32 bits.
+// Weights are rounded to the cache's type, which is what the matrix instruction takes; a second part for what that leaves off would be half as many products again.  Off by half
+// a step each, they are no further off than the result itself, which is rounded to the same type (the three shapes below against 64 bits: 2.7e-4, 2.8e-4 and, bf16, 2.2e-3
+// of the result, where rounding it alone gives 2.1e-4, 2.1e-4 and 1.7e-3).  Maxima, sums and results are in 32 bits.
 //
-// What bounds it: a wave's own chain of scores, maximum, weights and values, with two waves a SIMD (256 registers each).  8192 tokens of 32 heads and 128 dimensions, each at 16 pages of 64: 315 us; the
-// choices ask for 125 GFLOP, a wave's 8 tokens together for 181 (22 pages of the 64 in sight on average, the workgroup's 32 tokens for 27), so matrix units see 0.57 PFLOP/s, busy 24 % of the
-// cycles, vector instructions issuing in 37 %, waves waiting 38 %.  Not memory: with every entry naming the same page it takes as long.  Staging alone takes 155 us, lists, queries and results 48.
-// 1000 tokens of 64 heads of 64 dimensions behind 32768, 64 pages of 32 each: 149 us in three parts, of which 11 join them (33 GFLOP asked for, 46 done).  38 - 150 tokens of six short
-// sequences: 25 us, about 9 and 3 more for each 64 keys that follow each other.
-// What was worth it: waves leave out halves and 64 keys a tile in place of 32 with all waves at all of them 376 -> 315 and 207 -> 176, then parts 149.  And what was not: 8 waves for 256 pairs 348, two
+// What bounds it: a wave's own chain of scores, maximum, weights and values, with two waves a SIMD (256 registers each).  8192 tokens of 32 heads and 128 dimensions, each at 16 pages of 64: 307 - 315 us; the
+// choices ask for 125 GFLOP, a wave's 8 tokens together for 181 (22 pages of the 64 in sight on average, the workgroup's 32 tokens for 27), so matrix units see 0.58 PFLOP/s, busy 24 % of the
+// cycles, vector instructions issuing in 37 %, waves waiting 38 % (of launches under a profiler, which take 328 - 350 us).  Not memory: with every entry naming the same page it takes as long.  Staging alone takes 155 us, lists, queries and results 48.
+// 1000 tokens of 64 heads of 64 dimensions behind 32768, 64 pages of 32 each: 148 - 152 us in three parts, of which 11 join them (33 GFLOP asked for, 46 done).  38 - 150 tokens of six short
+// sequences: 25 us, about 9 and 3 more for each 64 keys that follow each other; attention over all of their pages (up to 368 tokens) takes 17, as it works on the next 32 keys' scores beside these.
+// Registers: two variants of 64 dimensions keep 6 and 12 of a lane's values in memory (pages of 64 tokens and more, pages of 16 and 32), one of 128 two (pages of 16 and 32), those of 256 dimensions 14 to 28;
+// staging holds 16, 32 or 64 registers beside the addresses and three tiles' places.
+// What was worth it: waves leave out halves and 64 keys a tile in place of 32 with all waves at all of them 376 -> 315 and 207 -> 176 (the six short ones stayed at 25), then parts 149.  And what was not: 8 waves for 256 pairs 348, two
 // tiles' halves in one stream of instructions 332, the next half's scores beside these weights 333, staging between halves 321, four halves deep 733 (registers in memory), 16 pairs
 // a wave on the 16x16 instruction with four waves a SIMD, which read every key and value twice as often, 2 % slower there and 13 % with 64 dimensions; priorities of waves make no difference.
 #include "paged_prompt.h"
