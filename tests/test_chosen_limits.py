@@ -16,7 +16,7 @@ def test_a_prompts_workspace_is_enough_for_smaller_batches(head_dim, kv_heads, q
               page_stride=head_dim * page_tokens * kv_heads)
     L, need = qkv.lib(), ctypes.c_uint64(0)
     per = 128 // (q_heads // kv_heads)
-    most = (4 * 768 // kv_heads + 2) * per
+    most = (3200 // kv_heads + 2) * per
     marks = sorted({max(1, n + d) for n in [1, per, 2 * per] + [most * i // 60 // per * per for i in range(61)] for d in (-1, 0, 1)})
     last, some = 0, False
     for at, tokens in enumerate(marks):
